@@ -341,7 +341,7 @@ def _run_adamw(s):
 
 
 def _mix32(x):
-    """A 32-bit mixing function (xor-shift and multiply, twice) on int64 values below 2^32."""
+    """A 32-bit mixing function (xor-shift and multiply, twice) on values below 2^32."""
     x = x ^ (x >> 16)
     x = x * 0x7FEB352D & 0xFFFFFFFF
     x = x ^ (x >> 15)
@@ -350,17 +350,21 @@ def _mix32(x):
 
 
 def _random32(n, tensor, step):
-    """The random 32 bits of each element of a tensor in a step."""
+    """The random 32 bits of each element of a tensor in a step: the two halves of a 64-bit product for every two elements."""
     k = _mix32(SEED & 0xFFFFFFFF)
     k = _mix32(k ^ (SEED >> 32))
     k = _mix32(k ^ (step & 0xFFFFFFFF))
     k = _mix32((k + tensor) & 0xFFFFFFFF)
-    i = torch.arange(n, device=DEVICE, dtype=torch.int64)
-    block = _mix32((k + (i // BLOCK) * 0x9E3779B9) & 0xFFFFFFFF)
-    return _mix32((block + (i % BLOCK) * 0x9E3779B9) & 0xFFFFFFFF)
+    i = torch.arange(0, n, 2, device=DEVICE, dtype=torch.int64)
+    x = _mix32((k + (i // BLOCK) * 0x9E3779B9) & 0xFFFFFFFF) + (i % BLOCK // 2) * 0x9E3779B9 & 0xFFFFFFFF
+    x = x ^ (x >> 16)
+    x = x * 0x7FEB352D & 0xFFFFFFFF
+    x = (x ^ (x >> 15)) * 0x846CA68B                                     # (wraps; its 64 bits are what counts)
+    low, high = x & 0xFFFFFFFF, x >> 32 & 0xFFFFFFFF
+    return torch.stack([low ^ high, high], -1).view(-1)[:n]
 
 
-def _random_q8(x, bits16):
+def _random_q8(x, bits20):
     """x [n] >= 0 or signed -> (codes, scales), each value rounded up or down to e4m3 with the probability that keeps its mean."""
     n = x.numel()
     rows = torch.nn.functional.pad(x, (0, -n % BLOCK)).view(-1, BLOCK)
@@ -371,7 +375,7 @@ def _random_q8(x, bits16):
     y = torch.where(bad[:, None], 0.0, y).view(-1)[:n]
     a = y.abs()
     low = a < 2.0 ** -6                                                  # below the normal numbers the step is 2^-9
-    code = (torch.where(low, a + 2.0 ** -6, a).view(torch.int32) + (bits16 * 16 + 8).to(torch.int32) >> 20) - torch.where(low, 121 << 3, 120 << 3)
+    code = (torch.where(low, a + 2.0 ** -6, a).view(torch.int32) + bits20.to(torch.int32) >> 20) - torch.where(low, 121 << 3, 120 << 3)
     return code.clamp_max(126), torch.signbit(y), y != 0, scale
 
 
@@ -407,10 +411,10 @@ def _plain_adamw(s):
         if q["copy"] is not None:
             _keep(q["copy"][i], new, ok)
         if c["state"] == "q8":
-            code, negative, _, scale = _random_q8(m, bits & 0xFFFF)
+            code, negative, _, scale = _random_q8(m, bits & 0xFFFFF)
             _keep(q["m"][i], code + negative.to(torch.int32) * 128, ok)
             _keep(q["ms"][i], scale, ok)
-            code, _, some, scale = _random_q8(v, bits >> 16)
+            code, _, some, scale = _random_q8(v, bits >> 12)
             _keep(q["v"][i], torch.where(some, code.clamp_min(1), code), ok)     # a second moment is never lost altogether
             _keep(q["vs"][i], scale, ok)
         else:
