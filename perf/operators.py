@@ -350,7 +350,7 @@ def _mix32(x):
 
 
 def _random32(n, tensor, step):
-    """The random 32 bits of each element of a tensor in a step: the two halves of a 64-bit product for every two elements."""
+    """The random 32 bits of each element of a tensor in a step: two neighbours share the first rounds of the mixing."""
     k = _mix32(SEED & 0xFFFFFFFF)
     k = _mix32(k ^ (SEED >> 32))
     k = _mix32(k ^ (step & 0xFFFFFFFF))
@@ -359,9 +359,9 @@ def _random32(n, tensor, step):
     x = _mix32((k + (i // BLOCK) * 0x9E3779B9) & 0xFFFFFFFF) + (i % BLOCK // 2) * 0x9E3779B9 & 0xFFFFFFFF
     x = x ^ (x >> 16)
     x = x * 0x7FEB352D & 0xFFFFFFFF
-    x = (x ^ (x >> 15)) * 0x846CA68B                                     # (wraps; its 64 bits are what counts)
-    low, high = x & 0xFFFFFFFF, x >> 32 & 0xFFFFFFFF
-    return torch.stack([low ^ high, high], -1).view(-1)[:n]
+    x = (x ^ (x >> 15)) * 0x846CA68B & 0xFFFFFFFF
+    y = x * 0xC2B2AE35 & 0xFFFFFFFF
+    return torch.stack([x ^ (x >> 16), y ^ (y >> 15)], -1).view(-1)[:n]
 
 
 def _random_q8(x, bits20):
