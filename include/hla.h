@@ -316,6 +316,149 @@ hla_status hla_timing_get(const hla_ctx *ctx, int32_t i, const char **name, doub
 
 hla_status hla_destroy(hla_ctx *ctx);
 
+/*
+ * Head preparation (Algorithm 1 steps 1-3: reshape to heads, rotary positions, scale), between a projection and
+ * hla_forward.  Every row x of d channels (one head of one token) becomes
+ *     y = s * R(theta) ( x / sqrt(mean(x^2) + eps) * w )
+ * with the RMS norm (norm = 1) and the scale (s = q_scale) on q, the norm on k, and neither norm, rotation nor scale on v.
+ * R turns the pairs of channels: pair p by theta = position[axis(p)] * inv_freq[p].  The first axis_width[0] / 2 pairs belong to axis
+ * 0 (the time of a video, say), the next axis_width[1] / 2 to axis 1, and so on; channels behind the last axis do not turn.
+ * HLA_PAIR_ADJACENT: pair p is the channels (2p, 2p+1).  HLA_PAIR_HALVES: the channels (p, p + R/2), R the sum of the
+ * widths.  Where inv_freq is NULL, pair j of an axis of n pairs has inv_freq = theta^(-j/n).  Angles are reduced in 64 bits: positions
+ * may be any int32.
+ * Positions: with a grid (row-major, its product N), token n is at its place in the grid plus start.  Without one
+ * (all of grid 0), or where a call is given `positions` (device int32 [B][N][n_axes], positions_batch_stride elements from one
+ * batch to the next, 0 for positions shared by all), they are read.
+ * Supported: d <= 128, rows and, for HLA_PAIR_HALVES, R in whole 16-byte pieces (d and R multiples of 8 in bf16, 4 in fp32),
+ * B*H <= 65535, B*N <= 2^28.  Sums and rotations are formed in fp32 and rounded once.
+ */
+typedef struct hla_heads hla_heads;
+typedef enum { HLA_PAIR_ADJACENT = 0, HLA_PAIR_HALVES = 1 } hla_pairing;
+typedef struct {
+    int32_t B, H, N, d;
+    int32_t dtype;         /* hla_dtype of all tensors and norm weights                                   */
+    int32_t pairing;       /* hla_pairing                                                                 */
+    int32_t norm;          /* 1: q and k are RMS-normalised per row                                       */
+    int32_t n_axes;        /* 0 (no rotation) to 3                                                        */
+    int32_t axis_width[3]; /* channels that turn with each axis: even, their sum <= d                     */
+    int32_t grid[3];       /* tokens along each axis, product N; all 0: every call is given positions     */
+    int32_t start[3];      /* position of the grid's first token                                          */
+    float eps;             /* 0 -> 1e-6                                                                   */
+    float q_scale;         /* 0 -> 1                                                                      */
+    double theta;          /* 0 -> 10000                                                                  */
+    const double *inv_freq; /* HOST array of one value per pair, copied; NULL: from theta                 */
+} hla_heads_config;
+
+/* A tensor [B][N][H][d] whose rows of H*d elements are contiguous: strides in elements, in whole 16-byte pieces (a
+ * projection [B][N][3][H][d] has token stride 3*H*d). */
+typedef struct {
+    const void *data;
+    int64_t batch_stride, token_stride;
+} hla_rows;
+typedef struct {
+    void *data;
+    int64_t batch_stride, token_stride;
+} hla_rows_out;
+
+hla_status hla_heads_create(const hla_heads_config *cfg, hla_heads **out);
+
+/* Scratch of hla_heads_backward (0 without norm; only needed where it is asked for dwq or dwk). */
+size_t hla_heads_workspace_bytes(const hla_heads *ctx);
+
+/* q, k, v -> Q, K, V [B][H][N][d], each may be NULL together with its output.  wq, wk: norm weights [d], NULL for ones.
+ * No output may lie within the memory that an input spans. */
+hla_status hla_heads_forward(hla_heads *ctx, const hla_rows *q, const hla_rows *k, const hla_rows *v, const void *wq, const void *wk,
+                             const int32_t *positions, int64_t positions_batch_stride, void *Q, void *K, void *V, void *cuda_stream);
+
+/*
+ * Gradients of sum(dQ Q + dK K + dV V): dq, dk, dv with strides of their own (so that they can be parts of one tensor that the
+ * projection's backward reads), and dwq, dwk (fp32 [d], overwritten; NULL: not wanted).  dQ, dK, dV may be NULL together with
+ * their outputs.  q and k are only read with norm = 1 and are the inputs of the forward.  The sums of dwq and dwk are formed
+ * in a fixed order.  dV alone moves a head-major tensor [B][H][N][d] to token-major rows, as an output projection reads them.
+ */
+hla_status hla_heads_backward(hla_heads *ctx, const void *dQ, const void *dK, const void *dV, const hla_rows *q, const hla_rows *k,
+                              const void *wq, const void *wk, const int32_t *positions, int64_t positions_batch_stride,
+                              const hla_rows_out *dq, const hla_rows_out *dk, const hla_rows_out *dv, void *dwq, void *dwk,
+                              void *workspace, size_t workspace_bytes, void *cuda_stream);
+hla_status hla_heads_destroy(hla_heads *ctx);
+
+/*
+ * AdamW step over many tensors (the update of a training step: the feature networks whose gradients hla_backward_weights
+ * leaves, and whatever else the model trains):
+ *     g = grad_scale * min(1, max_norm / (norm + 1e-6)) * grad,      norm = |grad_scale| * || all grads ||_2     (max_norm > 0)
+ *     m = beta1 m + (1 - beta1) g,    v = beta2 v + (1 - beta2) g^2
+ *     param = param - rate * weight_decay * param - rate * (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),  rate = lr * lr_mul
+ * With max_norm > 0 a step whose norm is not finite changes no tensor.
+ * Weights are fp32 or bf16, gradients fp32 or bf16, tensor by tensor.  fp32 weights may have a bf16 `copy`, rounded to nearest, for
+ * the kernels that read them; bf16 weights are rounded up or down at random with the probability that keeps the mean.
+ * HLA_STATE_F32: m, v fp32.  HLA_STATE_Q8: m, v are e4m3 codes (1 byte an element) with an fp32 scale for every 128
+ * elements of a tensor (m_scale, v_scale; the last scale may stand for fewer), scale = max |x| / 448; rounded at random like bf16
+ * weights, a positive second moment to a positive code.  A group whose largest entry is below 2^-100 is held as zeros; one with an
+ * entry that is not finite has a scale that is no number.  Random numbers are a function of seed, step, and the places of tensor and
+ * element: a step can be repeated bit for bit.  Zeros everywhere are the states before the first step.
+ */
+typedef struct hla_adamw hla_adamw;
+typedef enum { HLA_STATE_F32 = 0, HLA_STATE_Q8 = 1 } hla_state_type;
+typedef struct {
+    void *param, *copy;          /* copy: bf16, with fp32 weights only; may be NULL                    */
+    const void *grad;
+    void *m, *v;
+    void *m_scale, *v_scale;     /* fp32 [(n + 127) / 128], HLA_STATE_Q8 only                          */
+    int64_t n;                   /* elements; 0: the tensor is passed over                             */
+    float lr_mul;                /* 0 -> 1                                                             */
+    float weight_decay;
+    int32_t param_dtype, grad_dtype; /* hla_dtype                                                      */
+} hla_adamw_tensor;
+typedef struct {
+    double beta1, beta2, eps;    /* 0 <= beta < 1, eps > 0                                             */
+    int32_t state;               /* hla_state_type                                                     */
+    uint64_t seed;
+} hla_adamw_config;
+typedef struct {
+    double lr;
+    int64_t step;                /* the first step is 1                                                */
+    const float *lr_device;      /* device scalar that is read instead of lr, or NULL                  */
+    const int64_t *step_device;  /* device scalar that is read instead of step, or NULL: a captured step can be replayed with new values */
+    float max_norm;              /* 0: no norm is taken; infinity: the norm is taken and nothing is clipped */
+    float grad_scale;            /* 0 -> 1                                                             */
+    float *norm;                 /* device scalar that receives the norm (max_norm > 0), or NULL       */
+} hla_adamw_step_args;
+
+/* The pointers (16-byte aligned) are remembered; nothing that a step writes may share memory with another tensor of the list. */
+hla_status hla_adamw_create(const hla_adamw_config *cfg, const hla_adamw_tensor *tensors, int32_t n, hla_adamw **out);
+/* Other gradients (same types and sizes) from the next step on: one pointer per tensor of the list. */
+hla_status hla_adamw_set_grads(hla_adamw *ctx, const void *const *grads, int32_t n);
+size_t hla_adamw_workspace_bytes(const hla_adamw *ctx);      /* only needed by steps with max_norm > 0 */
+hla_status hla_adamw_step(hla_adamw *ctx, const hla_adamw_step_args *args, void *workspace, size_t workspace_bytes, void *cuda_stream);
+hla_status hla_adamw_destroy(hla_adamw *ctx);
+
+/*
+ * Gated linear recurrence (Section 4.4 "Causal Attention, Decay Factors and Sequential Updates", for a state of one value per
+ * channel): over the tokens of every sequence and for every channel
+ *     h_t = a_t h_{t-1} + u_t,     a_t = exp(g_t) (HLA_GATE_LOG, g_t <= 0) or 1 / (1 + exp(-g_t)) (HLA_GATE_SIGMOID),
+ *     u_t = x_t, or (1 - a_t) x_t with convex = 1.
+ * x, g [B][N][C] with strides (x and g may be parts of one projection); h, dh, dx, dg [B][N][C] contiguous and 16-byte aligned; states
+ * h0, h_last, dh_last, dh0 are fp32 [B][C] and may be NULL (zeros; not wanted).  A sequence that arrives in pieces is continued by
+ * passing the h_last of one call as the h0 of the next, the same buffer if wanted.  The state is carried in fp32, whatever the
+ * dtype.  The backward returns the gradients of sum(dh h) + sum(dh_last h_last) with respect to x, g and h0; h is the output of
+ * the forward.  x is only read there with convex = 1.  Outputs may not lie over inputs, but for dh0 over h0 or dh_last.
+ */
+typedef struct hla_scan hla_scan;
+typedef enum { HLA_GATE_LOG = 0, HLA_GATE_SIGMOID = 1 } hla_gate;
+typedef struct {
+    int32_t B, N, C;
+    int32_t dtype;                                   /* hla_dtype                              */
+    int32_t gate;                                    /* hla_gate                               */
+    int32_t convex;
+    int64_t x_batch_stride, x_token_stride;          /* elements; 0: contiguous                */
+    int64_t g_batch_stride, g_token_stride;
+} hla_scan_config;
+hla_status hla_scan_create(const hla_scan_config *cfg, hla_scan **out);
+hla_status hla_scan_forward(hla_scan *ctx, const void *x, const void *g, const void *h0, void *h, void *h_last, void *cuda_stream);
+hla_status hla_scan_backward(hla_scan *ctx, const void *x, const void *g, const void *h0, const void *h, const void *dh, const void *dh_last,
+                             void *dx, void *dg, void *dh0, void *cuda_stream);
+hla_status hla_scan_destroy(hla_scan *ctx);
+
 const char *hla_status_string(hla_status s);
 
 #ifdef __cplusplus

@@ -6,7 +6,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char_p, c_float, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 import torch
 
@@ -20,6 +20,9 @@ EXPORTS = [
     "hla_create", "hla_set_phi", "hla_workspace_bytes", "hla_workspace_layout", "hla_forward", "hla_backward", "hla_forward_keys", "hla_forward_queries", "hla_backward_queries", "hla_backward_keys", "hla_backward_weights", "hla_set_phi_v", "hla_set_carry", "hla_value_mod_forward", "hla_value_mod_backward", "hla_forward_static",
     "hla_last_device_status", "hla_selftest_bounded_wait", "hla_last_launch_count", "hla_timing_enable", "hla_timing_collect", "hla_timing_get",
     "hla_destroy", "hla_status_string",
+    "hla_heads_create", "hla_heads_workspace_bytes", "hla_heads_forward", "hla_heads_backward", "hla_heads_destroy",
+    "hla_adamw_create", "hla_adamw_set_grads", "hla_adamw_workspace_bytes", "hla_adamw_step", "hla_adamw_destroy",
+    "hla_scan_create", "hla_scan_forward", "hla_scan_backward", "hla_scan_destroy",
 ]
 
 
@@ -44,6 +47,40 @@ class HlaWsLayout(ctypes.Structure):
     _fields_ = [("status", c_size_t), ("qf", c_size_t), ("kf", c_size_t), ("state", c_size_t), ("eta", c_size_t),
                 ("dstate", c_size_t), ("dqf", c_size_t), ("dkf", c_size_t), ("state_ld", c_int32), ("state_rows", c_int32), ("n_splits", c_int32),
                 ("tensor_core", c_int32)]
+
+
+HLA_PAIR_ADJACENT, HLA_PAIR_HALVES = 0, 1
+HLA_STATE_F32, HLA_STATE_Q8 = 0, 1
+HLA_GATE_LOG, HLA_GATE_SIGMOID = 0, 1
+
+
+class HlaHeadsConfig(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("H", c_int32), ("N", c_int32), ("d", c_int32), ("dtype", c_int32), ("pairing", c_int32), ("norm", c_int32),
+                ("n_axes", c_int32), ("axis_width", c_int32 * 3), ("grid", c_int32 * 3), ("start", c_int32 * 3), ("eps", c_float), ("q_scale", c_float),
+                ("theta", c_double), ("inv_freq", POINTER(c_double))]
+
+
+class HlaRows(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("batch_stride", c_int64), ("token_stride", c_int64)]
+
+
+class HlaAdamwTensor(ctypes.Structure):
+    _fields_ = [("param", c_void_p), ("copy", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p), ("v_scale", c_void_p),
+                ("n", c_int64), ("lr_mul", c_float), ("weight_decay", c_float), ("param_dtype", c_int32), ("grad_dtype", c_int32)]
+
+
+class HlaAdamwConfig(ctypes.Structure):
+    _fields_ = [("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("state", c_int32), ("seed", c_uint64)]
+
+
+class HlaAdamwStepArgs(ctypes.Structure):
+    _fields_ = [("lr", c_double), ("step", c_int64), ("lr_device", c_void_p), ("step_device", c_void_p), ("max_norm", c_float), ("grad_scale", c_float),
+                ("norm", c_void_p)]
+
+
+class HlaScanConfig(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("N", c_int32), ("C", c_int32), ("dtype", c_int32), ("gate", c_int32), ("convex", c_int32),
+                ("x_batch_stride", c_int64), ("x_token_stride", c_int64), ("g_batch_stride", c_int64), ("g_token_stride", c_int64)]
 
 
 class HlaError(RuntimeError):
@@ -113,6 +150,25 @@ def load_library(rebuild: bool = False) -> ctypes.CDLL:
     lib.hla_timing_get.restype = c_int32
     lib.hla_destroy.argtypes = [c_void_p]
     lib.hla_destroy.restype = c_int32
+    for name, args in {
+        "hla_heads_create": [POINTER(HlaHeadsConfig), POINTER(c_void_p)],
+        "hla_heads_forward": [c_void_p] * 7 + [c_int64] + [c_void_p] * 4,
+        "hla_heads_backward": [c_void_p] * 9 + [c_int64] + [c_void_p] * 6 + [c_size_t, c_void_p],
+        "hla_heads_destroy": [c_void_p],
+        "hla_adamw_create": [POINTER(HlaAdamwConfig), POINTER(HlaAdamwTensor), c_int32, POINTER(c_void_p)],
+        "hla_adamw_set_grads": [c_void_p, POINTER(c_void_p), c_int32],
+        "hla_adamw_step": [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p],
+        "hla_adamw_destroy": [c_void_p],
+        "hla_scan_create": [POINTER(HlaScanConfig), POINTER(c_void_p)],
+        "hla_scan_forward": [c_void_p] * 7,
+        "hla_scan_backward": [c_void_p] * 11,
+        "hla_scan_destroy": [c_void_p],
+    }.items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = c_int32
+    for name in ("hla_heads_workspace_bytes", "hla_adamw_workspace_bytes"):
+        getattr(lib, name).argtypes = [c_void_p]
+        getattr(lib, name).restype = c_size_t
     lib.hla_status_string.argtypes = [c_int32]
     lib.hla_status_string.restype = c_char_p
     _lib = lib
@@ -397,3 +453,318 @@ class Hla:
             self.close()
         except Exception:
             pass
+
+
+# ---- operators beside the attention ------------------------------------------
+_DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+_CODES = {torch.bfloat16: HLA_BF16, torch.float32: HLA_F32}
+
+
+def _dtype(name):
+    if name not in _DTYPES:
+        raise ValueError(f"dtype {name!r}: 'bf16' or 'f32' is wanted")
+    return _DTYPES[name]
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _device() -> int:
+    """The current device: work is enqueued on its current stream."""
+    return _current_device() if _current_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device() if torch.cuda.is_available() else 0
+
+
+def _here(t, what, dtype, shape=None, device=None):
+    """A tensor on the current device of the given type and shape."""
+    device = _device() if device is None else device
+    if t.dtype is dtype and (shape is None or t.shape == shape) and t.get_device() == device:
+        return t
+    if t.dtype is not dtype:
+        raise ValueError(f"{what}: {dtype} is wanted, not {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{what}: shape {tuple(shape)} is wanted, not {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: a CUDA tensor is wanted")
+    raise ValueError(f"{what}: on {t.device}, but the current device is cuda:{device}")
+
+
+def _dense(t, what, dtype, shape=None, device=None):
+    if t is None:
+        return 0
+    _here(t, what, dtype, shape, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: must be contiguous")
+    return t.data_ptr()
+
+
+class _Owner:
+    """Holds a context of the library until it is closed or collected."""
+    ctx, _destroy = None, ""
+
+    def close(self):
+        if self.ctx:
+            getattr(load_library(), self._destroy)(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _create(name, *args) -> int:
+    out = c_void_p()
+    st = getattr(load_library(), name)(*args, byref(out))
+    if st != HLA_OK:
+        raise HlaError(st, name)
+    return out.value
+
+
+class Heads(_Owner):
+    """Head preparation around a projection (hla_heads_*): RMS norm of the rows of q and k, rotation by up to three axes, scale of q, and
+    the move from [B,N,H,d] (any token stride: parts of one projection) to the [B,H,N,d] that Hla takes; and its backward.
+
+    axes: channels that turn with each axis.  grid: tokens along each axis (None: every call is given `positions`, int32 [N, axes] or
+    [B, N, axes]).  inv_freq: one value per pair (None: theta ** (-j / n) for pair j of an axis of n pairs)."""
+    _destroy = "hla_heads_destroy"
+
+    def __init__(self, B, H, N, d, dtype="bf16", axes=(), grid=None, start=(0, 0, 0), theta=10000.0, inv_freq=None, pairing="interleaved", norm=False,
+                 eps=1e-6, q_scale=1.0, device="cuda"):
+        if pairing not in ("interleaved", "half"):
+            raise ValueError(f"pairing {pairing!r}: 'interleaved' or 'half' is wanted")
+        if len(axes) > 3 or (grid is not None and len(grid) != len(axes)):
+            raise ValueError("up to three axes, and a grid of as many")
+        if inv_freq is not None and len(inv_freq) != sum(axes) // 2:
+            raise ValueError(f"inv_freq: {sum(axes) // 2} values are wanted, not {len(inv_freq)}")
+        if float(q_scale) == 0.0 or not theta > 0.0:
+            raise ValueError("q_scale must not be 0, and theta must be positive")
+        three = lambda v: (c_int32 * 3)(*[int(x) for x in v])  # noqa: E731
+        freq = (c_double * len(inv_freq))(*[float(f) for f in inv_freq]) if inv_freq is not None else None
+        self.torch_dtype = _dtype(dtype)
+        self.cfg = HlaHeadsConfig(B, H, N, d, _CODES[self.torch_dtype], HLA_PAIR_HALVES if pairing == "half" else HLA_PAIR_ADJACENT, 1 if norm else 0,
+                                  len(axes), three(axes), three(grid or ()), three(start), eps, q_scale, theta, freq)
+        self.ctx = _create("hla_heads_create", byref(self.cfg))
+        self.cfg.inv_freq = None            # (copied by the library)
+        self.device = device
+        self._rows, self._out, self._weight = torch.Size((B, N, H, d)), torch.Size((B, H, N, d)), torch.Size((d,))
+        self._need = int(load_library().hla_heads_workspace_bytes(self.ctx))
+        self.workspace = torch.empty(self._need, dtype=torch.uint8, device=device) if device and self._need else None
+        self._scratch = _ptr(self.workspace)
+        rows = [HlaRows() for _ in range(6)]
+        self._slots = [(what, r, byref(r)) for what, r in zip(("q", "k", "v", "dq", "dk", "dv"), rows)]
+        self._forward, self._backward = load_library().hla_heads_forward, load_library().hla_heads_backward
+
+    def _strided(self, t, slot, device):
+        """The tensor's place and strides for the library, in a slot of its own (reused: a context serves one call at a time)."""
+        what, row, at = self._slots[slot]
+        _here(t, what, self.torch_dtype, self._rows, device)
+        sb, sn, sh, sd = t.stride()
+        H, d = self.cfg.H, self.cfg.d
+        if (sd != 1 and d > 1) or (sh != d and H > 1):
+            raise ValueError(f"{what}: the {H} x {d} channels of a token must be contiguous")
+        row.data, row.batch_stride, row.token_stride = t.data_ptr(), sb, sn
+        return at
+
+    def _positions(self, p, device):
+        if p is None:
+            return 0, 0
+        B, N = self.cfg.B, self.cfg.N
+        shape = (N, self.cfg.n_axes) if p.dim() == 2 else (B, N, self.cfg.n_axes)
+        return _dense(p, "positions", torch.int32, torch.Size(shape), device), 0 if p.dim() == 2 else N * self.cfg.n_axes
+
+    def forward(self, q=None, k=None, v=None, wq=None, wk=None, positions=None, Q=None, K=None, V=None, stream=None):
+        """q, k, v [B,N,H,d] (None: left out) -> Q, K, V [B,H,N,d].  wq, wk: norm weights [d] (None: ones)."""
+        dt, dev, shape = self.torch_dtype, _device(), self._out
+        rows, outs, at = [None] * 3, [Q, K, V], [0] * 3
+        for i, t in enumerate((q, k, v)):
+            if t is not None:
+                rows[i] = self._strided(t, i, dev)
+                if outs[i] is None:
+                    outs[i] = torch.empty(shape, dtype=dt, device=t.device)
+                    at[i] = outs[i].data_ptr()
+                    continue
+            at[i] = _dense(outs[i], "output", dt, shape, dev)
+        pos, pos_batch = self._positions(positions, dev)
+        st = self._forward(self.ctx, rows[0], rows[1], rows[2], _dense(wq, "wq", dt, self._weight, dev), _dense(wk, "wk", dt, self._weight, dev), pos, pos_batch,
+                           at[0], at[1], at[2], _stream(stream))
+        if st != HLA_OK:
+            raise HlaError(st, "hla_heads_forward")
+        return outs
+
+    def backward(self, dQ=None, dK=None, dV=None, q=None, k=None, v=None, dq=None, dk=None, dv=None, wq=None, wk=None, positions=None, dwq=None, dwk=None,
+                 stream=None):
+        """Writes the gradients of q, k, v into dq, dk, dv (views [B,N,H,d]; only where dQ, dK, dV are given) and returns those of the norm
+        weights (fp32 [d]; None without norm).  v is accepted next to q and k and not read."""
+        dt, dev, f32 = self.torch_dtype, _device(), torch.float32
+        norm = self.cfg.norm == 1
+        x = [self._strided(t, i, dev) if norm and t is not None else None for i, t in enumerate((q, k))]
+        out = [self._strided(t, 3 + i, dev) if t is not None else None for i, t in enumerate((dq, dk, dv))]
+        if norm and dQ is not None and dwq is None:
+            dwq = torch.empty(self._weight, dtype=f32, device=dQ.device)
+        if norm and dK is not None and dwk is None:
+            dwk = torch.empty(self._weight, dtype=f32, device=dK.device)
+        pos, pos_batch = self._positions(positions, dev)
+        shape, w = self._out, self._weight
+        st = self._backward(self.ctx, _dense(dQ, "dQ", dt, shape, dev), _dense(dK, "dK", dt, shape, dev), _dense(dV, "dV", dt, shape, dev), x[0], x[1],
+                            _dense(wq, "wq", dt, w, dev), _dense(wk, "wk", dt, w, dev), pos, pos_batch, out[0], out[1], out[2], _dense(dwq, "dwq", f32, w, dev),
+                            _dense(dwk, "dwk", f32, w, dev), self._scratch, self._need, _stream(stream))
+        if st != HLA_OK:
+            raise HlaError(st, "hla_heads_backward")
+        return dwq, dwk
+
+
+class AdamW(_Owner):
+    """One AdamW step over a list of tensors (hla_adamw_*).  params: fp32 or bf16; grads: fp32 or bf16, read where they are at every step
+    (set_grads names others); copies: bf16 copies of fp32 params that a step rewrites.  state: "f32", or "q8" for moments of one byte with a scale
+    per 128 elements.  ms, vs (and m_scales, v_scales) are made with zeros where they are not given.  weight_decay, lr_mul: a number, or one for each tensor.
+    norm: fp32 scalar that receives the norm of the gradients in steps with max_norm > 0 (made where not given)."""
+    _destroy = "hla_adamw_destroy"
+
+    def __init__(self, params, grads, ms=None, vs=None, m_scales=None, v_scales=None, copies=None, state=None, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0,
+                 lr_mul=1.0, seed=0, norm=None, device="cuda"):
+        n = len(params)
+        state = state or ("q8" if ms and ms[0].dtype is torch.uint8 else "f32")
+        if state not in ("f32", "q8"):
+            raise ValueError(f"state {state!r}: 'f32' or 'q8' is wanted")
+        q8 = state == "q8"
+        kind, groups = torch.uint8 if q8 else torch.float32, lambda p: (p.numel() + 127) // 128
+        make = lambda size, dt: [torch.zeros(size(p), dtype=dt, device=p.device) for p in params]  # noqa: E731
+        ms = make(torch.Tensor.numel, kind) if ms is None else ms
+        vs = make(torch.Tensor.numel, kind) if vs is None else vs
+        if q8:
+            m_scales = make(groups, torch.float32) if m_scales is None else m_scales
+            v_scales = make(groups, torch.float32) if v_scales is None else v_scales
+        each = lambda v: [float(x) for x in v] if hasattr(v, "__len__") else [float(v)] * n  # noqa: E731
+        decay, mul = each(weight_decay), each(lr_mul)
+        for what, v in (("grads", grads), ("ms", ms), ("vs", vs), ("m_scales", m_scales), ("v_scales", v_scales), ("copies", copies), ("weight_decay", decay), ("lr_mul", mul)):
+            if v is not None and len(v) != n:
+                raise ValueError(f"{what}: one for each of the {n} params is wanted, not {len(v)}")
+        if any(x == 0.0 for x in mul):
+            raise ValueError("lr_mul must not be 0: leave out tensors that are not trained")
+        rows = (HlaAdamwTensor * n)()
+        for i, p in enumerate(params):
+            if p.dtype not in _CODES or grads[i].dtype not in _CODES:
+                raise ValueError(f"params[{i}], grads[{i}]: torch.float32 or torch.bfloat16 is wanted")
+            size, rows_of = p.numel(), groups(p)
+            count = lambda t, what, dt, k: 0 if t is None else _dense(t, f"{what}[{i}]", dt) if t.numel() == k else self._wrong(what, i, k, t)  # noqa: E731
+            rows[i] = HlaAdamwTensor(_dense(p, f"params[{i}]", p.dtype), count(copies[i] if copies else None, "copies", torch.bfloat16, size),
+                                     count(grads[i], "grads", grads[i].dtype, size), count(ms[i], "ms", kind, size), count(vs[i], "vs", kind, size),
+                                     count(m_scales[i], "m_scales", torch.float32, rows_of) if q8 else 0, count(v_scales[i], "v_scales", torch.float32, rows_of) if q8 else 0,
+                                     size, mul[i], decay[i], _CODES[p.dtype], _CODES[grads[i].dtype])
+        self.norm = torch.zeros((), dtype=torch.float32, device=device) if norm is None else norm
+        _dense(self.norm, "norm", torch.float32)
+        cfg = HlaAdamwConfig(betas[0], betas[1], eps, HLA_STATE_Q8 if q8 else HLA_STATE_F32, seed)
+        self.ctx = _create("hla_adamw_create", byref(cfg), rows, n)
+        # the library only borrows pointers
+        self.params, self.grads, self.ms, self.vs, self.m_scales, self.v_scales, self.copies = params, grads, ms, vs, m_scales, v_scales, copies
+        self.steps = 0
+        self._need = int(load_library().hla_adamw_workspace_bytes(self.ctx))
+        self.workspace = torch.empty(self._need, dtype=torch.uint8, device=device)
+        self._scratch, self._on, self._norm = self.workspace.data_ptr(), self.norm.get_device(), self.norm.data_ptr()
+        self._step = load_library().hla_adamw_step
+
+    @staticmethod
+    def _wrong(what, i, k, t):
+        raise ValueError(f"{what}[{i}]: {k} elements are wanted, not {t.numel()}")
+
+    def set_grads(self, grads):
+        if len(grads) != len(self.grads):
+            raise ValueError(f"grads: {len(self.grads)} are wanted, not {len(grads)}")
+        for i, (new, old) in enumerate(zip(grads, self.grads)):
+            _dense(new, f"grads[{i}]", old.dtype)
+            if new.numel() != old.numel():
+                self._wrong("grads", i, old.numel(), new)
+        st = load_library().hla_adamw_set_grads(self.ctx, (c_void_p * len(grads))(*[g.data_ptr() for g in grads]), len(grads))
+        if st != HLA_OK:
+            raise HlaError(st, "hla_adamw_set_grads")
+        self.grads = grads
+
+    def step(self, lr, step=None, max_norm=0.0, grad_scale=1.0, stream=None):
+        """lr: a number, or an fp32 CUDA scalar that the step reads.  step: its number from 1 on (None: counted here), or an int64 CUDA scalar: with
+        both on the device a captured step can be replayed with new values."""
+        if grad_scale == 0.0:
+            raise ValueError("grad_scale must not be 0")
+        a = HlaAdamwStepArgs(0.0, 1, 0, 0, max_norm, grad_scale, self._norm)
+        if isinstance(lr, torch.Tensor):
+            a.lr_device = _dense(lr, "lr", torch.float32)
+        else:
+            a.lr = lr
+        if isinstance(step, torch.Tensor):
+            a.step_device = _dense(step, "step", torch.int64)
+        else:
+            a.step = self.steps + 1 if step is None else step
+        if self._on != _device():
+            raise ValueError(f"the tensors are on {self.workspace.device}, but the current device is cuda:{_device()}")
+        st = self._step(self.ctx, byref(a), self._scratch, self._need, _stream(stream))
+        if st != HLA_OK:
+            raise HlaError(st, "hla_adamw_step")
+        if not isinstance(step, torch.Tensor):
+            self.steps = a.step
+
+
+class Scan(_Owner):
+    """Gated linear recurrence h_t = a_t h_{t-1} + u_t over tokens (hla_scan_*), a = exp(g) (gate "log") or sigmoid(g) (gate "sigmoid"), u = x or, with
+    convex, (1 - a) x; and its backward.  x, g [B,N,C], channels contiguous; states are fp32 [B,C]."""
+    _destroy = "hla_scan_destroy"
+
+    def __init__(self, B, N, C, dtype="bf16", gate="log", convex=False, device="cuda"):
+        if gate not in ("log", "sigmoid"):
+            raise ValueError(f"gate {gate!r}: 'log' or 'sigmoid' is wanted")
+        self.torch_dtype = _dtype(dtype)
+        self.cfg = HlaScanConfig(B, N, C, _CODES[self.torch_dtype], HLA_GATE_SIGMOID if gate == "sigmoid" else HLA_GATE_LOG, 1 if convex else 0, 0, 0, 0, 0)
+        self._make()
+        self._made_for = None
+        self.device = device
+        self._shape, self._state = torch.Size((B, N, C)), torch.Size((B, C))
+        self._forward, self._backward = load_library().hla_scan_forward, load_library().hla_scan_backward
+
+    def _make(self):
+        new = _create("hla_scan_create", byref(self.cfg))
+        self.close()
+        self.ctx = new
+
+    def _strides(self, x, g, device):
+        """Follows the strides of x and g (a context has those it was made for)."""
+        B, N, C = self._shape
+        want = []
+        for t, what in ((x, "x"), (g, "g")):
+            _here(t, what, self.torch_dtype, self._shape, device)
+            sb, sn, sc = t.stride()
+            if sc != 1 and C > 1:
+                raise ValueError(f"{what}: the channels of a token must be contiguous")
+            if (N > 1 and sn < C) or (B > 1 and sb < C):
+                raise ValueError(f"{what}: tokens must not share memory")
+            sn = sn if N > 1 else C
+            want += [sb if B > 1 else N * sn, sn]
+        if want != self._made_for:
+            c = self.cfg
+            c.x_batch_stride, c.x_token_stride, c.g_batch_stride, c.g_token_stride = want
+            self._make()
+            self._made_for = want
+
+    def forward(self, x, g, h0=None, h=None, h_last=None, stream=None):
+        """h [B,N,C] and the state behind the last token.  h_last may be the tensor h0."""
+        dev, f32 = _device(), torch.float32
+        self._strides(x, g, dev)
+        h = torch.empty(self._shape, dtype=self.torch_dtype, device=x.device) if h is None else h
+        h_last = torch.empty(self._state, dtype=f32, device=x.device) if h_last is None else h_last
+        st = self._forward(self.ctx, x.data_ptr(), g.data_ptr(), _dense(h0, "h0", f32, self._state, dev), _dense(h, "h", self.torch_dtype, self._shape, dev),
+                           _dense(h_last, "h_last", f32, self._state, dev), _stream(stream))
+        if st != HLA_OK:
+            raise HlaError(st, "hla_scan_forward")
+        return h, h_last
+
+    def backward(self, x, g, h, dh, h0=None, dlast=None, dx=None, dg=None, stream=None):
+        """dx, dg [B,N,C] and, where h0 is given, its gradient (else None).  h: what forward returned; dlast: gradient of the state behind the last token."""
+        dev, f32, dt, shape = _device(), torch.float32, self.torch_dtype, self._shape
+        self._strides(x, g, dev)
+        dx = torch.empty(shape, dtype=dt, device=x.device) if dx is None else dx
+        dg = torch.empty(shape, dtype=dt, device=x.device) if dg is None else dg
+        dh0 = torch.empty(self._state, dtype=f32, device=x.device) if h0 is not None else None
+        st = self._backward(self.ctx, x.data_ptr(), g.data_ptr(), _dense(h0, "h0", f32, self._state, dev), _dense(h, "h", dt, shape, dev),
+                            _dense(dh, "dh", dt, shape, dev), _dense(dlast, "dlast", f32, self._state, dev), _dense(dx, "dx", dt, shape, dev),
+                            _dense(dg, "dg", dt, shape, dev), 0 if dh0 is None else dh0.data_ptr(), _stream(stream))
+        if st != HLA_OK:
+            raise HlaError(st, "hla_scan_backward")
+        return dx, dg, dh0

@@ -1,0 +1,594 @@
+// One AdamW step over many tensors, with moments in fp32 or in 8 bits, and the global gradient norm it is clipped by.
+//
+//     m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2,   p' = p - lr wd p - lr / (1 - b1^t) m' / (sqrt(v' / (1 - b2^t)) + eps)
+//
+// What bounds it: memory (28 bytes an element with fp32 weights and moments and bf16 gradients, 10 with bf16 weights and 8-bit moments,
+// where the arithmetic comes close: about 45 instructions an element).
+//
+// Layout: a warp takes rows of 128 consecutive elements of a tensor, four per lane, so that every load of a row is contiguous whatever
+// the type (16 bytes a lane in fp32, 8 in bf16, 4 in 8 bits) and a row is also what shares a scale.  Tensors from a few weights to
+// millions are cut into chunks of 16 rows; a launch knows up to kMany tensors from its parameters alone (nothing to upload, a
+// captured step holds it) and its blocks go through the chunks in order.
+//
+// 8-bit moments: e4m3 codes of x / scale, scale = max |x| of the row / 448.  Rounded up or down at random with the probability that
+// keeps the mean: a second moment changes by a thousandth of itself a step, a sixty-fourth to a hundred-and-twenty-eighth of the step
+// between two codes, and rounding to the nearest would leave it where it is for ever.  A positive second moment never becomes zero (the
+// quotient would explode): its code is at least 1.  bf16 weights without an fp32 original are rounded in the same way.
+#include "../../include/hla.h"
+
+#include <math.h>
+
+#include <algorithm>
+#include <memory>
+#include <new>
+#include <vector>
+
+#include <cuda_fp16.h>
+
+#include "hla_ops_common.cuh"
+
+namespace hla {
+namespace adamw {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kRow = 128;                        // elements of a row: a scale of the 8-bit states
+constexpr int kRows = 2;                         // rows of a warp per chunk
+constexpr int kChunk = kWarps * kRows * kRow;
+constexpr int kFew = 40, kMany = 360;            // tensors per launch: 3.7 and 32 KB of parameters
+constexpr float kDead = 7.888609052210118e-31f;  // 2^-100: a row whose largest entry is below is held as zeros (its scale could not be inverted)
+
+struct Tensor {
+    void *p, *copy;
+    const void* g;
+    void *m, *v;
+    float *ms, *vs;
+    long long n;
+    float lr_mul, decay;
+    uint32_t first;      // its first chunk in the launch
+    uint32_t number;     // its place in the caller's list
+    uint16_t p_bf16, g_bf16;
+};
+
+template <int MANY>
+struct Args {
+    int n;                        // tensors of this launch
+    uint32_t chunks;
+    int norm_blocks;              // partial sums of the squared norm (0: no norm)
+    double* part;
+    float* norm_out;
+    float max_norm, grad_scale;
+    float b1, r1, b2, r2, eps;
+    double beta1, beta2;
+    float lr, inv1, inv2;         // 1 / (1 - b1^t) and (1 - b2^t)^(-1/2) where the step is known on the host
+    long long step;
+    const float* lr_device;
+    const long long* step_device;
+    uint32_t seed_lo, seed_hi;
+    Tensor t[MANY];
+};
+
+__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
+    x ^= x >> 16;
+    x *= 0x7FEB352Du;
+    x ^= x >> 15;
+    x *= 0x846CA68Bu;
+    return x ^ (x >> 16);
+}
+
+// The tensor that chunk c belongs to, from the one that an earlier chunk belonged to on.
+template <int MANY>
+__device__ __forceinline__ int tensor_of(const Args<MANY>& a, uint32_t c, int from) {
+    if (from + 1 >= a.n || c < a.t[from + 1].first) return from;
+    int lo = from + 1, hi = a.n;      // first[lo] <= c < first[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        (c < a.t[mid].first ? hi : lo) = mid;
+    }
+    return lo;
+}
+
+// Four elements at `i` of a tensor with `n` elements in all, as raw words; elements behind the end are zeros.
+template <bool NC>
+__device__ __forceinline__ uint4 load_f32(const void* base, long long i, long long n) {
+    const float* p = static_cast<const float*>(base) + i;
+    if (i + 4 <= n) return NC ? ld_once(reinterpret_cast<const uint4*>(p)) : *reinterpret_cast<const uint4*>(p);
+    uint4 r = make_uint4(0, 0, 0, 0);
+    if (i < n) r.x = __float_as_uint(p[0]);
+    if (i + 1 < n) r.y = __float_as_uint(p[1]);
+    if (i + 2 < n) r.z = __float_as_uint(p[2]);
+    return r;
+}
+template <bool NC>
+__device__ __forceinline__ uint2 load_bf16(const void* base, long long i, long long n) {
+    const unsigned short* p = static_cast<const unsigned short*>(base) + i;
+    if (i + 4 <= n) return NC ? ld_once(reinterpret_cast<const uint2*>(p)) : *reinterpret_cast<const uint2*>(p);
+    uint2 r = make_uint2(0, 0);
+    if (i < n) r.x = p[0];
+    if (i + 1 < n) r.x |= (uint32_t)p[1] << 16;
+    if (i + 2 < n) r.y = p[2];
+    return r;
+}
+__device__ __forceinline__ uint32_t load_b8(const void* base, long long i, long long n) {
+    const unsigned char* p = static_cast<const unsigned char*>(base) + i;
+    if (i + 4 <= n) return *reinterpret_cast<const uint32_t*>(p);
+    uint32_t r = 0;
+    if (i < n) r = p[0];
+    if (i + 1 < n) r |= (uint32_t)p[1] << 8;
+    if (i + 2 < n) r |= (uint32_t)p[2] << 16;
+    return r;
+}
+// Four floats or bf16 values; the type is a property of the tensor (the same for a whole block).
+template <bool NC>
+__device__ __forceinline__ uint4 load_any(const void* base, bool bf16, long long i, long long n) {
+    if (bf16) {
+        const uint2 r = load_bf16<NC>(base, i, n);
+        return make_uint4(r.x, r.y, 0, 0);
+    }
+    return load_f32<NC>(base, i, n);
+}
+__device__ __forceinline__ void unpack(const uint4& r, bool bf16, float (&x)[4]) {
+    if (bf16) {
+        x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xffff0000u);
+        x[2] = __uint_as_float(r.y << 16); x[3] = __uint_as_float(r.y & 0xffff0000u);
+    } else {
+        x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+    }
+}
+__device__ __forceinline__ void store_f32(void* base, long long i, long long n, const float (&x)[4]) {
+    float* p = static_cast<float*>(base) + i;
+    if (i + 4 <= n) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); return; }
+    for (int j = 0; j < 3; ++j)
+        if (i + j < n) p[j] = x[j];
+}
+__device__ __forceinline__ void store_bf16(void* base, long long i, long long n, uint32_t lo, uint32_t hi) {
+    unsigned short* p = static_cast<unsigned short*>(base) + i;
+    if (i + 4 <= n) { *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi); return; }
+    if (i < n) p[0] = (unsigned short)lo;
+    if (i + 1 < n) p[1] = (unsigned short)(lo >> 16);
+    if (i + 2 < n) p[2] = (unsigned short)hi;
+}
+__device__ __forceinline__ void store_b8(void* base, long long i, long long n, uint32_t c) {
+    unsigned char* p = static_cast<unsigned char*>(base) + i;
+    if (i + 4 <= n) { *reinterpret_cast<uint32_t*>(p) = c; return; }
+    if (i < n) p[0] = (unsigned char)c;
+    if (i + 1 < n) p[1] = (unsigned char)(c >> 8);
+    if (i + 2 < n) p[2] = (unsigned char)(c >> 16);
+}
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Two e4m3 codes as floats (exact).
+__device__ __forceinline__ void decode2(uint32_t codes, float& x, float& y) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)codes));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    x = f.x;
+    y = f.y;
+}
+
+__device__ __forceinline__ float max_abs(float a, float b) {      // a NaN stays
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
+
+// The largest of a row's |x| from every lane's own four; not a number if one of them is none.
+__device__ __forceinline__ float row_max(const float (&x)[4]) {
+    const float most = max_abs(max_abs(max_abs(fabsf(x[0]), x[1]), x[2]), x[3]);
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));      // (bits of non-negative floats are ordered like them)
+}
+
+// A value as e4m3, rounded by the 20 random bits `r`, in the top byte of the result.  x * inv is at most 448; times 2^-120 the smallest
+// normal e4m3 falls on the smallest normal fp32, so that one addition to the bits rounds normal and subnormal codes alike.
+__device__ __forceinline__ uint32_t round_q8(float x, float inv, uint32_t r) {
+    const uint32_t w = __float_as_uint(__fmul_rn(__fmul_rn(x, inv), 7.52316384526264e-37f)) + r;
+    return (w & 0x80000000u) | (w << 4);
+}
+__device__ __forceinline__ uint32_t top_bytes(const uint32_t (&w)[4]) {
+    return __byte_perm(__byte_perm(w[0], w[1], 0x0073), __byte_perm(w[2], w[3], 0x0073), 0x5410);
+}
+
+// The scale of a row whose largest entry is `most`.  A row with an entry that is no number, or infinite, is no numbers throughout.
+__device__ __forceinline__ float scale_of(float most) {
+    if (most < kDead) return 0.f;
+    return most <= 3.402823466e38f ? most / 448.f : __int_as_float(0x7fc00000);
+}
+
+__device__ __forceinline__ float sqrt_fast(float x) {
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// The sum of the partial sums of the squared norm, in a fixed order, to every thread.
+__device__ __forceinline__ double block_total(const double* part, int count, double* scratch) {
+    double v = 0.0;
+    for (int i = threadIdx.x; i < count; i += kThreads) v += part[i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.0;
+    for (int w = 0; w < kWarps; ++w) v += scratch[w];
+    return v;
+}
+
+// Squares are summed in 64 bits: large gradients cannot overflow the sum, and a step does not depend on how it was cut.
+template <int MANY>
+__global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ Args<MANY> a) {
+    __shared__ double scratch[kWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    double sum = 0.0;
+    int at = 0;
+    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+        at = tensor_of(a, c, at);
+        const Tensor& t = a.t[at];
+        const long long first = (long long)(c - t.first) * kChunk + warp * (kRows * kRow) + lane * 4;
+        uint4 raw[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) raw[r] = load_any<false>(t.g, t.g_bf16, first + r * kRow, t.n);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            float g[4];
+            unpack(raw[r], t.g_bf16, g);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum = fma((double)g[j], (double)g[j], sum);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) scratch[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0.0;
+        for (int w = 0; w < kWarps; ++w) sum += scratch[w];
+        a.part[blockIdx.x] = sum;
+    }
+}
+
+template <int MANY, bool Q8>
+__global__ void __launch_bounds__(kThreads, 4) step_kernel(const __grid_constant__ Args<MANY> a) {
+    __shared__ double scratch[kWarps];
+    __shared__ float hyper[2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    wait_for_previous_kernel();
+    const long long step = a.step_device ? *a.step_device : a.step;
+    if (a.step_device && threadIdx.x == 0) {
+        hyper[0] = (float)(-1.0 / expm1((double)step * log(a.beta1)));
+        hyper[1] = (float)rsqrt(-expm1((double)step * log(a.beta2)));
+    }
+    float gain = a.grad_scale;
+    if (a.norm_blocks) {
+        const float norm = (float)(sqrt(block_total(a.part, a.norm_blocks, scratch)) * fabs((double)a.grad_scale));
+        if (blockIdx.x == 0 && threadIdx.x == 0 && a.norm_out) *a.norm_out = norm;
+        if (!isfinite(norm)) return;      // nothing changes
+        gain *= fminf(a.max_norm / (norm + 1e-6f), 1.f);
+    }
+    __syncthreads();
+    const float lr = a.lr_device ? *a.lr_device : a.lr;
+    const float inv1 = a.step_device ? hyper[0] : a.inv1, inv2 = a.step_device ? hyper[1] : a.inv2;
+    const uint32_t key = mix32(mix32(mix32(a.seed_lo) ^ a.seed_hi) ^ (uint32_t)step);
+    int at = 0;
+    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+        at = tensor_of(a, c, at);
+        const Tensor& t = a.t[at];
+        const long long n = t.n, row0 = (long long)(c - t.first) * (kWarps * kRows) + warp * kRows, first = row0 * kRow + lane * 4;
+        const bool pb = t.p_bf16, gb = t.g_bf16;
+        uint4 rg[kRows], rp[kRows], rm[kRows], rv[kRows];
+        uint32_t cm[kRows], cv[kRows];
+        float sm[kRows], sv[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const long long i = first + r * kRow;
+            rg[r] = load_any<false>(t.g, gb, i, n);
+            rp[r] = load_any<false>(t.p, pb, i, n);
+            if (Q8) {
+                const bool some = (row0 + r) * kRow < n;
+                cm[r] = load_b8(t.m, i, n);
+                cv[r] = load_b8(t.v, i, n);
+                sm[r] = some ? t.ms[row0 + r] : 0.f;
+                sv[r] = some ? t.vs[row0 + r] : 0.f;
+            } else {
+                rm[r] = load_f32<false>(t.m, i, n);
+                rv[r] = load_f32<false>(t.v, i, n);
+            }
+        }
+        const float rate = lr * t.lr_mul, size = rate * inv1, shrink = rate * t.decay;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const long long i = first + r * kRow;
+            float g[4], p[4], m[4], v[4];
+            unpack(rg[r], gb, g);
+            unpack(rp[r], pb, p);
+            if (Q8) {
+                decode2(cm[r], m[0], m[1]); decode2(cm[r] >> 16, m[2], m[3]);
+                decode2(cv[r], v[0], v[1]); decode2(cv[r] >> 16, v[2], v[3]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { m[j] *= sm[r]; v[j] *= sv[r]; }
+            } else {
+                unpack(rm[r], false, m);
+                unpack(rv[r], false, v);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g[j] *= gain;
+                m[j] = __fadd_rn(__fmul_rn(a.b1, m[j]), __fmul_rn(a.r1, g[j]));
+                v[j] = __fadd_rn(__fmul_rn(a.b2, v[j]), __fmul_rn(__fmul_rn(a.r2, g[j]), g[j]));
+                const float root = sqrt_fast(v[j]);
+                p[j] = fmaf(-shrink, p[j], p[j]) - size * __fdividef(m[j], fmaf(root, inv2, a.eps));
+            }
+            uint32_t bits[4];
+            if (Q8 || pb) {
+                const uint32_t block = mix32(mix32(key + t.number) + (uint32_t)(row0 + r) * 0x9E3779B9u);
+#pragma unroll
+                for (int j = 0; j < 4; j += 2) {
+                    uint32_t x = block + (uint32_t)(lane * 2 + j / 2) * 0x9E3779B9u;
+                    x ^= x >> 16;
+                    x *= 0x7FEB352Du;
+                    x = (x ^ (x >> 15)) * 0x846CA68Bu;
+                    const uint32_t y = x * 0xC2B2AE35u;
+                    bits[j] = x ^ (x >> 16);
+                    bits[j + 1] = y ^ (y >> 15);
+                }
+            }
+            if (pb) {
+                uint32_t h[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t w = __float_as_uint(p[j]);
+                    h[j] = (w & 0x7f800000u) == 0x7f800000u ? w : w + (bits[j] * 0x9E3779B9u >> 16);
+                }
+                store_bf16(t.p, i, n, __byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x7632));
+            } else {
+                store_f32(t.p, i, n, p);
+            }
+            if (t.copy) store_bf16(t.copy, i, n, two_bf16(p[0], p[1]), two_bf16(p[2], p[3]));
+            if (!Q8) {
+                store_f32(t.m, i, n, m);
+                store_f32(t.v, i, n, v);
+            } else {
+                const float mm = row_max(m), mv = row_max(v);
+                uint32_t qm = 0, qv = 0;
+                if (mm >= kDead && mm <= 3.402823466e38f) {
+                    const float inv = __fdiv_rz(448.f, mm);
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = round_q8(m[j], inv, bits[j] & 0xfffffu);
+                    qm = top_bytes(w);
+                }
+                if (mv >= kDead && mv <= 3.402823466e38f) {
+                    const float inv = __fdiv_rz(448.f, mv);
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = max(round_q8(v[j], inv, bits[j] >> 12), v[j] > 0.f ? 1u << 24 : 0u);
+                    qv = top_bytes(w);
+                }
+                store_b8(t.m, i, n, qm);
+                store_b8(t.v, i, n, qv);
+                if (lane == 0 && i < n) {
+                    t.ms[row0 + r] = scale_of(mm);
+                    t.vs[row0 + r] = scale_of(mv);
+                }
+            }
+        }
+    }
+}
+
+}  // namespace adamw
+}  // namespace hla
+
+using namespace hla;
+
+struct hla_adamw {
+    hla_adamw_config cfg;
+    std::vector<adamw::Tensor> t;      // those with weights in them; `first` within their launch
+    int given;
+    int sm_count;
+};
+
+namespace {
+
+struct Span {
+    uintptr_t at, end;
+    bool written;
+};
+
+// Whether one of the tensors that a step writes shares memory with another one.
+bool clash(std::vector<Span>& spans) {
+    std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
+    uintptr_t end = 0, written = 0;      // how far the spans so far reach, all and the written ones
+    for (const Span& s : spans) {
+        if (s.at < (s.written ? end : written)) return true;
+        end = std::max(end, s.end);
+        if (s.written) written = std::max(written, s.end);
+    }
+    return false;
+}
+
+hla_status check_spans(const hla_adamw* c) {
+    const bool q8 = c->cfg.state == HLA_STATE_Q8;
+    std::vector<Span> spans;
+    auto add = [&](const void* p, long long bytes, bool written) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p) spans.push_back({at, at + (uintptr_t)bytes, written});
+    };
+    for (const adamw::Tensor& t : c->t) {
+        const long long rows = (t.n + adamw::kRow - 1) / adamw::kRow;
+        add(t.p, t.n * (t.p_bf16 ? 2 : 4), true);
+        add(t.copy, t.n * 2, true);
+        add(t.m, t.n * (q8 ? 1 : 4), true);
+        add(t.v, t.n * (q8 ? 1 : 4), true);
+        if (q8) add(t.ms, rows * 4, true), add(t.vs, rows * 4, true);
+        add(t.g, t.n * (t.g_bf16 ? 2 : 4), false);
+    }
+    return clash(spans) ? HLA_ERR_INVALID_ARG : HLA_OK;
+}
+
+template <int MANY>
+void fill(adamw::Args<MANY>& a, const hla_adamw* c, int from, int n) {
+    a.n = n;
+    a.chunks = 0;
+    for (int i = 0; i < n; ++i) {
+        a.t[i] = c->t[from + i];
+        a.t[i].first = a.chunks;
+        a.chunks += (uint32_t)((a.t[i].n + adamw::kChunk - 1) / adamw::kChunk);
+    }
+}
+
+// Tensors from `from` on that one launch takes.
+int batch(const hla_adamw* c, int from) {
+    const int left = (int)c->t.size() - from;
+    return left < adamw::kMany ? left : adamw::kMany;
+}
+
+int norm_blocks(const hla_adamw* c, uint32_t chunks) { return (int)std::min<uint32_t>(chunks, 8u * c->sm_count); }
+
+template <typename A>
+bool launch_step(void (*kern)(A), dim3 blocks, const A& a, cudaStream_t st) {
+    if (a.norm_blocks) return launch_behind(kern, blocks, adamw::kThreads, st, a);
+    kern<<<blocks, adamw::kThreads, 0, st>>>(a);
+    return cudaGetLastError() == cudaSuccess;
+}
+
+template <int MANY>
+hla_status step(const hla_adamw* c, const hla_adamw_step_args& s, double* part, cudaStream_t st) {
+    adamw::Args<MANY> a;
+    const hla_adamw_config& k = c->cfg;
+    a.part = part;
+    a.norm_out = s.norm;
+    a.max_norm = s.max_norm;
+    a.grad_scale = s.grad_scale == 0.f ? 1.f : s.grad_scale;
+    a.b1 = (float)k.beta1; a.r1 = (float)(1.0 - k.beta1);
+    a.b2 = (float)k.beta2; a.r2 = (float)(1.0 - k.beta2);
+    a.eps = (float)k.eps;
+    a.beta1 = k.beta1; a.beta2 = k.beta2;
+    a.lr = (float)s.lr;
+    a.step = s.step;
+    a.inv1 = s.step_device ? 0.f : (float)(-1.0 / expm1((double)s.step * log(k.beta1)));
+    a.inv2 = s.step_device ? 0.f : (float)(1.0 / sqrt(-expm1((double)s.step * log(k.beta2))));
+    a.lr_device = s.lr_device;
+    a.step_device = reinterpret_cast<const long long*>(s.step_device);
+    a.seed_lo = (uint32_t)k.seed;
+    a.seed_hi = (uint32_t)(k.seed >> 32);
+    a.norm_blocks = 0;
+    const int total = (int)c->t.size();
+    if (s.max_norm > 0.f) {
+        for (int from = 0; from < total; from += batch(c, from)) {
+            fill(a, c, from, batch(c, from));
+            const int blocks = norm_blocks(c, a.chunks);
+            a.part = part + a.norm_blocks;
+            adamw::norm_kernel<MANY><<<blocks, adamw::kThreads, 0, st>>>(a);
+            if (cudaGetLastError() != cudaSuccess) return HLA_ERR_CUDA;
+            a.norm_blocks += blocks;
+        }
+        a.part = part;
+    }
+    for (int from = 0; from < total; from += batch(c, from)) {
+        fill(a, c, from, batch(c, from));
+        if (from) a.norm_out = nullptr;
+        const dim3 blocks(std::min<uint32_t>(a.chunks, 4u * c->sm_count));
+        const bool ok = k.state == HLA_STATE_Q8 ? launch_step(adamw::step_kernel<MANY, true>, blocks, a, st) : launch_step(adamw::step_kernel<MANY, false>, blocks, a, st);
+        if (!ok) return HLA_ERR_CUDA;
+    }
+    return HLA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+hla_status hla_adamw_create(const hla_adamw_config* cfg, const hla_adamw_tensor* tensors, int32_t n, hla_adamw** out) {
+    if (out) *out = nullptr;
+    if (!cfg || !out || !tensors || n <= 0) return HLA_ERR_INVALID_ARG;
+    if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !(cfg->eps > 0.0) || !((float)cfg->eps > 0.f) || !isfinite(cfg->eps))
+        return HLA_ERR_INVALID_ARG;
+    if (cfg->state != HLA_STATE_F32 && cfg->state != HLA_STATE_Q8) return HLA_ERR_INVALID_ARG;
+    const bool q8 = cfg->state == HLA_STATE_Q8;
+    if (n > (1 << 20)) return HLA_ERR_UNSUPPORTED;
+    try {
+        std::unique_ptr<hla_adamw> c(new hla_adamw());
+        c->cfg = *cfg;
+        c->given = n;
+        c->sm_count = current_sm_count();
+        hla_status st = HLA_OK;
+        unsigned long long chunks = 0;
+        for (int i = 0; i < n && st == HLA_OK; ++i) {
+            const hla_adamw_tensor& t = tensors[i];
+            if (t.n < 0 || (t.param_dtype != HLA_BF16 && t.param_dtype != HLA_F32) || (t.grad_dtype != HLA_BF16 && t.grad_dtype != HLA_F32) ||
+                !isfinite(t.lr_mul) || !isfinite(t.weight_decay)) { st = HLA_ERR_INVALID_ARG; break; }
+            if (t.n == 0) continue;
+            const void* all[] = {t.param, t.grad, t.m, t.v, q8 ? t.m_scale : t.m, q8 ? t.v_scale : t.v};
+            for (const void* p : all)
+                if (!p || !aligned16(p)) st = HLA_ERR_INVALID_ARG;
+            if (!aligned16(t.copy) || (t.copy && t.param_dtype != HLA_F32)) st = HLA_ERR_INVALID_ARG;
+            if (t.n > (1ll << 38)) st = HLA_ERR_UNSUPPORTED;
+            chunks += (unsigned long long)(t.n + adamw::kChunk - 1) / adamw::kChunk;
+            adamw::Tensor d{};
+            d.p = t.param; d.copy = t.copy; d.g = t.grad; d.m = t.m; d.v = t.v;
+            d.ms = q8 ? static_cast<float*>(t.m_scale) : nullptr;
+            d.vs = q8 ? static_cast<float*>(t.v_scale) : nullptr;
+            d.n = t.n;
+            d.number = (uint32_t)i;
+            d.lr_mul = t.lr_mul == 0.f ? 1.f : t.lr_mul;
+            d.decay = t.weight_decay;
+            d.p_bf16 = t.param_dtype == HLA_BF16;
+            d.g_bf16 = t.grad_dtype == HLA_BF16;
+            c->t.push_back(d);
+        }
+        if (st == HLA_OK && chunks >= (1ull << 31)) st = HLA_ERR_UNSUPPORTED;
+        if (st == HLA_OK) st = check_spans(c.get());
+        if (st == HLA_OK) *out = c.release();
+        return st;
+    } catch (...) {
+        return HLA_ERR_NO_MEMORY;
+    }
+}
+
+hla_status hla_adamw_set_grads(hla_adamw* c, const void* const* grads, int32_t n) {
+    if (!c || !grads || n != c->given) return HLA_ERR_INVALID_ARG;
+    for (const adamw::Tensor& t : c->t)
+        if (!grads[t.number] || !aligned16(grads[t.number])) return HLA_ERR_INVALID_ARG;
+    try {
+        std::vector<adamw::Tensor> before = c->t;
+        for (adamw::Tensor& t : c->t) t.g = grads[t.number];
+        const hla_status st = check_spans(c);
+        if (st != HLA_OK) c->t.swap(before);
+        return st;
+    } catch (...) {
+        return HLA_ERR_NO_MEMORY;
+    }
+}
+
+size_t hla_adamw_workspace_bytes(const hla_adamw* c) {
+    if (!c) return 0;
+    size_t n = 0;
+    for (int from = 0; from < (int)c->t.size(); from += batch(c, from)) n += (size_t)8 * c->sm_count;
+    return (n * 8 + 255) / 256 * 256;
+}
+
+hla_status hla_adamw_step(hla_adamw* c, const hla_adamw_step_args* s, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!c || !s) return HLA_ERR_INVALID_ARG;
+    if (!(s->max_norm >= 0.f) || !isfinite(s->grad_scale) || !isfinite(s->lr)) return HLA_ERR_INVALID_ARG;
+    if (!s->step_device && s->step < 1) return HLA_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(s->step_device) & 7u) || (reinterpret_cast<uintptr_t>(s->lr_device) & 3u) || (reinterpret_cast<uintptr_t>(s->norm) & 3u))
+        return HLA_ERR_INVALID_ARG;
+    if (c->t.empty())      // nothing but a norm of nothing
+        return s->max_norm > 0.f && s->norm && cudaMemsetAsync(s->norm, 0, 4, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess ? HLA_ERR_CUDA : HLA_OK;
+    if (s->max_norm > 0.f) {
+        if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
+        if (workspace_bytes < hla_adamw_workspace_bytes(c)) return HLA_ERR_WORKSPACE;
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    double* part = static_cast<double*>(workspace);
+    return (int)c->t.size() <= adamw::kFew ? step<adamw::kFew>(c, *s, part, st) : step<adamw::kMany>(c, *s, part, st);
+}
+
+hla_status hla_adamw_destroy(hla_adamw* c) {
+    if (!c) return HLA_ERR_INVALID_ARG;
+    delete c;
+    return HLA_OK;
+}
+
+}  // extern "C"

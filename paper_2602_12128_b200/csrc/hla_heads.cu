@@ -1,0 +1,611 @@
+// Head preparation: what a projection [B,N,H,d] needs before it enters hla_forward (Algorithm 1 steps 1-3), and its backward.
+//
+//     y = s R(theta_n) (x r . w),   r = (mean x^2 + eps)^(-1/2),   theta_{n,p} = position_{axis(p)} inv_freq_p
+//     g = s R(-theta_n) dy,   dw = sum g . x r,   dx = r (g . w - x r mean(g . w . x r))
+//
+// What bounds it: memory.  A row of d channels is read once (the backward: dy and x), about ten operations an element, and
+// written once, at another place: the rows of one token lie together in the projection, those of one head in Q, K, V.
+//
+// Layout: 16 bytes of a row per lane, so a row of 128 bf16 channels is half a warp and is summed with four shuffles; the two
+// channels of every pair are in the same lane in both pairings.  Such a group of lanes takes one token and goes through the
+// heads of one tensor: the angles of a token (a product and a reduction in 64 bits, one sincospi per pair) are computed once and
+// stay in registers.  Neighbouring groups take neighbouring tokens, so a block reads rows of H d and writes runs of 16 tokens.
+#include "../../include/hla.h"
+
+#include <math.h>
+#include <new>
+
+#include "hla_ops_common.cuh"
+
+namespace hla {
+namespace heads {
+
+constexpr int kThreads = 256;
+constexpr int kMaxPairs = kMaxD / 2;
+constexpr int kDwThreads = 1024;
+
+struct Tensor {
+    const char *x, *dy;          // projection (strided); gradient of the prepared tensor (head-major)
+    char* out;                   // forward: prepared tensor (head-major); backward: gradient of the projection (strided)
+    long long x_batch, x_token, o_batch, o_token;    // strides in bytes; o_* of the backward's output
+    const void* w;
+    float scale;
+    int rotate;                  // 0: the rows are only moved
+};
+
+struct Args {
+    double turns[kMaxPairs];     // turns of a pair per unit of position
+    int pair_end[3];             // first pair behind each axis; pairs behind the last do not turn
+    int grid[3], stride[3], start[3], n_axes;
+    const int* positions;
+    long long pos_batch;         // elements
+    int B, H, N, d;
+    int log_lanes;
+    int rot_lanes;               // lanes that hold rotated pairs of the half-split pairing; further lanes hold 16 bytes of the rest
+    int half;                    // offset of the second channel of a pair of the half-split pairing
+    float eps, inv_d;
+    int n_tensors, chunks, per_chunk;                // every tensor's heads in `chunks` runs of `per_chunk`
+    Tensor t[3];
+    float* part;                 // [tensor][chunk, block][d] partial sums of the weight gradients
+    int want_dw;
+};
+
+// 16 bytes of a row as NP pairs of fp32.  Adjacent pairing: 16 consecutive bytes; half-split: 8 bytes at either place.
+template <typename T, bool HALF> struct Vec;
+template <bool HALF> struct Vec<__nv_bfloat16, HALF> {
+    static constexpr int CH = 8, NP = 4;
+    static __device__ __forceinline__ void unpack(const uint4& r, float (&a)[4], float (&b)[4]) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xffff0000u);
+            if (!HALF) { a[i] = lo; b[i] = hi; }
+            else if (i < 2) { a[2 * i] = lo; a[2 * i + 1] = hi; }
+            else { b[2 * i - 4] = lo; b[2 * i - 3] = hi; }
+        }
+    }
+    static __device__ __forceinline__ uint32_t two(float lo, float hi) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&a)[4], const float (&b)[4]) {
+        if (!HALF) return make_uint4(two(a[0], b[0]), two(a[1], b[1]), two(a[2], b[2]), two(a[3], b[3]));
+        return make_uint4(two(a[0], a[1]), two(a[2], a[3]), two(b[0], b[1]), two(b[2], b[3]));
+    }
+};
+template <bool HALF> struct Vec<float, HALF> {
+    static constexpr int CH = 4, NP = 2;
+    static __device__ __forceinline__ void unpack(const uint4& r, float (&a)[2], float (&b)[2]) {
+        a[0] = __uint_as_float(r.x);
+        (HALF ? a[1] : b[0]) = __uint_as_float(r.y);
+        (HALF ? b[0] : a[1]) = __uint_as_float(r.z);
+        b[1] = __uint_as_float(r.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&a)[2], const float (&b)[2]) {
+        return make_uint4(__float_as_uint(a[0]), __float_as_uint(HALF ? a[1] : b[0]), __float_as_uint(HALF ? b[0] : a[1]), __float_as_uint(b[1]));
+    }
+};
+
+// Where a lane's 16 bytes of a row are: off_a and off_b in bytes (off_b only counts in the half-split pairing).
+template <typename T, bool HALF>
+struct Place {
+    int off_a, off_b;
+    bool in;      // the lane has channels
+    __device__ __forceinline__ Place(const Args& p, int l) {
+        constexpr int CH = Vec<T, HALF>::CH, NP = Vec<T, HALF>::NP;
+        in = l * CH < p.d;
+        if (HALF && l < p.rot_lanes) {
+            off_a = l * NP * (int)sizeof(T);
+            off_b = off_a + p.half * (int)sizeof(T);
+        } else {
+            off_a = l * 16;
+            off_b = off_a + 8;
+        }
+    }
+    __device__ __forceinline__ uint4 load(const char* row) const {
+        uint4 r;
+        if (HALF) {
+            const uint2 a = ld_once(reinterpret_cast<const uint2*>(row + off_a)), b = ld_once(reinterpret_cast<const uint2*>(row + off_b));
+            r = make_uint4(a.x, a.y, b.x, b.y);
+        } else {
+            r = ld_once(reinterpret_cast<const uint4*>(row + off_a));
+        }
+        return r;
+    }
+    __device__ __forceinline__ void store(char* row, const uint4& r) const {
+        if (HALF) {
+            *reinterpret_cast<uint2*>(row + off_a) = make_uint2(r.x, r.y);
+            *reinterpret_cast<uint2*>(row + off_b) = make_uint2(r.z, r.w);
+        } else {
+            *reinterpret_cast<uint4*>(row + off_a) = r;
+        }
+    }
+};
+
+// cos and sin of a lane's pairs at token n of batch b, times `scale`.  The angle is reduced to a fraction of a turn in 64 bits: at
+// position 2^31 its error is below 2^-22 turns.
+template <typename T, bool HALF>
+__device__ __forceinline__ void angles(const Args& p, const double* turns, int l, int b, int n, float scale, float (&c)[Vec<T, HALF>::NP], float (&s)[Vec<T, HALF>::NP]) {
+    constexpr int NP = Vec<T, HALF>::NP;
+    int pos[3] = {0, 0, 0};
+#pragma unroll
+    for (int a = 0; a < 3; ++a)
+        if (a < p.n_axes) pos[a] = p.positions ? p.positions[b * p.pos_batch + (long long)n * p.n_axes + a] : n / p.stride[a] % p.grid[a] + p.start[a];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int pair = l * NP + i;
+        c[i] = scale;
+        s[i] = 0.f;
+        if (pair < p.pair_end[2]) {
+            const double x = (double)(pair < p.pair_end[0] ? pos[0] : pair < p.pair_end[1] ? pos[1] : pos[2]) * turns[pair];
+            float sn, cs;
+            sincospif(2.f * (float)(x - rint(x)), &sn, &cs);
+            c[i] = cs * scale;
+            s[i] = sn * scale;
+        }
+    }
+}
+
+__device__ __forceinline__ float lanes_sum(float v, int log_lanes) {
+    for (int o = 1 << log_lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+template <typename T, bool HALF, bool NORM>
+__global__ void __launch_bounds__(kThreads) forward_kernel(const __grid_constant__ Args p) {
+    using V = Vec<T, HALF>;
+    constexpr int NP = V::NP, U = 4;
+    __shared__ double turns[kMaxPairs];
+    if (threadIdx.x < kMaxPairs) turns[threadIdx.x] = p.turns[threadIdx.x];
+    __syncthreads();
+    const int l = threadIdx.x & ((1 << p.log_lanes) - 1);
+    const uint32_t tokens = (uint32_t)p.B * p.N, units = tokens * p.n_tensors * p.chunks;
+    uint32_t unit = blockIdx.x * (uint32_t)(kThreads >> p.log_lanes) + (threadIdx.x >> p.log_lanes);
+    const bool live = unit < units;
+    if (!live) unit = 0;      // (stays for the shuffles of its warp)
+    const uint32_t run = unit / tokens, token = unit - run * tokens;
+    const int b = token / p.N, n = token - b * p.N;
+    const Tensor& t = p.t[run / p.chunks];
+    const int h0 = (run % p.chunks) * p.per_chunk, h1 = min(p.H, h0 + p.per_chunk);
+    const Place<T, HALF> at(p, l);
+    const bool mine = live && at.in;
+    const size_t row = (size_t)p.d * sizeof(T), head = row * p.N;
+    const char* src = t.x + b * t.x_batch + n * t.x_token + h0 * row;
+    char* dst = t.out + ((size_t)b * p.H + h0) * head + n * row;
+
+    float c[NP], s[NP], wa[NP], wb[NP];
+    if (t.rotate) {
+        angles<T, HALF>(p, turns, l, b, n, t.scale, c, s);
+        if (NORM) {
+            uint4 w = {};
+            if (t.w && mine) { w = at.load(static_cast<const char*>(t.w)); }
+            V::unpack(w, wa, wb);
+            if (!t.w) {
+#pragma unroll
+                for (int i = 0; i < NP; ++i) wa[i] = wb[i] = 1.f;
+            }
+        }
+    }
+    for (int h = 0; h < p.per_chunk; h += U) {
+        uint4 r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            r[u] = make_uint4(0, 0, 0, 0);
+            if (mine && h0 + h + u < h1) r[u] = at.load(src + (h + u) * row);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (h + u >= p.per_chunk) break;
+            if (t.rotate) {
+                float a[NP], v[NP];
+                V::unpack(r[u], a, v);
+                if (NORM) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) ss += a[i] * a[i] + v[i] * v[i];
+                    const float q = rsqrtf(lanes_sum(ss, p.log_lanes) * p.inv_d + p.eps);
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) { a[i] = a[i] * q * wa[i]; v[i] = v[i] * q * wb[i]; }
+                }
+                float ya[NP], yb[NP];
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    ya[i] = a[i] * c[i] - v[i] * s[i];
+                    yb[i] = a[i] * s[i] + v[i] * c[i];
+                }
+                r[u] = V::pack(ya, yb);
+            }
+            if (mine && h0 + h + u < h1) at.store(dst + (size_t)(h + u) * head, r[u]);
+        }
+    }
+}
+
+// A block stays with one run of heads of one tensor (blockIdx.y) and goes through tokens, so that its sums for the weight gradient
+// can stay in registers until the end.
+template <typename T, bool HALF, bool NORM>
+__global__ void __launch_bounds__(kThreads) backward_kernel(const __grid_constant__ Args p) {
+    using V = Vec<T, HALF>;
+    constexpr int NP = V::NP, U = 2;
+    __shared__ double turns[kMaxPairs];
+    __shared__ float sums[kThreads * 2 * NP];
+    if (threadIdx.x < kMaxPairs) turns[threadIdx.x] = p.turns[threadIdx.x];
+    __syncthreads();
+    const int l = threadIdx.x & ((1 << p.log_lanes) - 1), groups = kThreads >> p.log_lanes, group = threadIdx.x >> p.log_lanes;
+    const int ti = blockIdx.y / p.chunks, chunk = blockIdx.y % p.chunks;
+    const Tensor& t = p.t[ti];
+    const int h0 = chunk * p.per_chunk, h1 = min(p.H, h0 + p.per_chunk);
+    const Place<T, HALF> at(p, l);
+    const size_t row = (size_t)p.d * sizeof(T), head = row * p.N;
+    const uint32_t tokens = (uint32_t)p.B * p.N;
+    float wa[NP], wb[NP], da[NP], db[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) { wa[i] = wb[i] = 1.f; da[i] = db[i] = 0.f; }
+    if (NORM && t.rotate && t.w) {
+        uint4 w = {};
+        if (at.in) w = at.load(static_cast<const char*>(t.w));
+        V::unpack(w, wa, wb);
+    }
+    for (uint32_t first = blockIdx.x * groups; first < tokens; first += gridDim.x * groups) {
+        const bool live = first + group < tokens;
+        const uint32_t token = live ? first + group : first;
+        const int b = token / p.N, n = token - b * p.N;
+        const bool mine = live && at.in;
+        const char* dy = t.dy + ((size_t)b * p.H + h0) * head + n * row;
+        const char* src = t.x + b * t.x_batch + n * t.x_token + h0 * row;
+        char* dst = t.out + b * t.o_batch + n * t.o_token + h0 * row;
+        float c[NP], s[NP];
+        if (t.rotate) angles<T, HALF>(p, turns, l, b, n, t.scale, c, s);
+        for (int h = 0; h < p.per_chunk; h += U) {
+            uint4 r[U], x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                r[u] = x[u] = make_uint4(0, 0, 0, 0);
+                if (mine && h0 + h + u < h1) {
+                    r[u] = at.load(dy + (size_t)(h + u) * head);
+                    if (NORM && t.rotate) x[u] = at.load(src + (h + u) * row);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (h + u >= p.per_chunk) break;
+                if (t.rotate) {
+                    float ya[NP], yb[NP], ga[NP], gb[NP];
+                    V::unpack(r[u], ya, yb);
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {
+                        ga[i] = ya[i] * c[i] + yb[i] * s[i];
+                        gb[i] = yb[i] * c[i] - ya[i] * s[i];
+                    }
+                    if (NORM) {
+                        float xa[NP], xb[NP], ss = 0.f, gx = 0.f;
+                        V::unpack(x[u], xa, xb);
+#pragma unroll
+                        for (int i = 0; i < NP; ++i) {
+                            ss += xa[i] * xa[i] + xb[i] * xb[i];
+                            gx += ga[i] * wa[i] * xa[i] + gb[i] * wb[i] * xb[i];
+                        }
+                        const float q = rsqrtf(lanes_sum(ss, p.log_lanes) * p.inv_d + p.eps);
+                        const float m = lanes_sum(gx, p.log_lanes) * q * p.inv_d;
+#pragma unroll
+                        for (int i = 0; i < NP; ++i) {
+                            const float ha = xa[i] * q, hb = xb[i] * q;
+                            da[i] += ga[i] * ha;
+                            db[i] += gb[i] * hb;
+                            ga[i] = q * (ga[i] * wa[i] - ha * m);
+                            gb[i] = q * (gb[i] * wb[i] - hb * m);
+                        }
+                    }
+                    r[u] = V::pack(ga, gb);
+                }
+                if (mine && h0 + h + u < h1) at.store(dst + (h + u) * row, r[u]);
+            }
+        }
+    }
+    if (NORM && p.want_dw && t.rotate) {      // (uniform over the block)
+        // group after group: sums[group][channel]
+        constexpr int CH = V::CH;
+        float* mine = sums + (size_t)group * CH * (1 << p.log_lanes);
+        if (at.in) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int ca = HALF ? at.off_a / (int)sizeof(T) + i : l * CH + 2 * i, cb = HALF ? at.off_b / (int)sizeof(T) + i : ca + 1;
+                mine[ca] = da[i];
+                mine[cb] = db[i];
+            }
+        }
+        __syncthreads();
+        float* part = p.part + ((size_t)(ti * p.chunks + chunk) * gridDim.x + blockIdx.x) * p.d;
+        for (int ch = threadIdx.x; ch < p.d; ch += kThreads) {
+            float v = 0.f;
+            for (int g = 0; g < groups; ++g) v += sums[(size_t)g * CH * (1 << p.log_lanes) + ch];
+            part[ch] = v;
+        }
+    }
+}
+
+// Sums the partial rows of one tensor (blockIdx.y) for 32 channels (blockIdx.x) in a fixed order.
+__global__ void __launch_bounds__(kDwThreads) dw_kernel(const float* part, int rows, int d, float* dw0, float* dw1) {
+    __shared__ double sums[32][33];
+    const int ch = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
+    wait_for_previous_kernel();
+    const float* mine = part + (size_t)blockIdx.y * rows * d;
+    double v = 0.0;
+    if (ch < d)
+        for (int r = slice; r < rows; r += 32) v += mine[(size_t)r * d + ch];
+    sums[slice][threadIdx.x & 31] = v;
+    __syncthreads();
+    if (slice == 0 && ch < d) {
+        for (int i = 1; i < 32; ++i) v += sums[i][threadIdx.x];
+        float* dw = blockIdx.y ? dw1 : dw0;
+        if (dw) dw[ch] = (float)v;
+    }
+}
+
+}  // namespace heads
+}  // namespace hla
+
+using namespace hla;
+
+struct hla_heads {
+    hla_heads_config cfg;
+    double turns[heads::kMaxPairs];
+    int pair_end[3], rot;          // rotated channels
+    bool grid_known;
+    int log_lanes, sm_count;
+};
+
+namespace {
+
+int elt_size(int dtype) { return dtype == HLA_BF16 ? 2 : 4; }
+
+// Tokens of the grid-stride loop that one block of the backward takes at a time, and how many blocks share the tokens.
+int backward_blocks(const hla_heads* c, int y) {
+    const long long tokens = (long long)c->cfg.B * c->cfg.N;
+    const int groups = heads::kThreads >> c->log_lanes;
+    const long long tiles = (tokens + groups - 1) / groups;
+    // four waves of four resident blocks: V's blocks, which read half as much, make room early
+    const long long want = (16ll * c->sm_count + y - 1) / y;
+    return (int)(tiles < want ? tiles : want);
+}
+
+// Heads that one group of lanes goes through.  All of a tensor's where the tokens alone fill the machine (the angles of a token are
+// computed once per run); single heads for a few tokens.
+int heads_per_run(const hla_heads* c, int tensors) {
+    const long long tokens = (long long)c->cfg.B * c->cfg.N;
+    const int groups = heads::kThreads >> c->log_lanes;
+    int chunks = 1;
+    while (chunks < c->cfg.H && tokens * tensors * chunks < 4ll * c->sm_count * groups) chunks *= 2;
+    if (chunks > c->cfg.H) chunks = c->cfg.H;
+    return (c->cfg.H + chunks - 1) / chunks;
+}
+
+bool rows_ok(const hla_heads* c, const hla_rows* r) {
+    const long long elt = elt_size(c->cfg.dtype);
+    if (!r->data || (reinterpret_cast<uintptr_t>(r->data) & 15u)) return false;
+    const long long width = (long long)c->cfg.H * c->cfg.d;
+    const bool tokens = c->cfg.N > 1, batches = c->cfg.B > 1;      // a stride of one step is never taken
+    if (tokens && (r->token_stride < width || r->token_stride > (1ll << 40) || (r->token_stride * elt & 15))) return false;
+    if (batches && (r->batch_stride < (tokens ? (c->cfg.N - 1) * r->token_stride : 0) + width || r->batch_stride > (1ll << 56) || (r->batch_stride * elt & 15))) return false;
+    return true;
+}
+
+size_t rows_span(const hla_heads* c, const hla_rows* r) {
+    return (size_t)((c->cfg.B > 1 ? (c->cfg.B - 1) * r->batch_stride : 0) + (c->cfg.N > 1 ? (c->cfg.N - 1) * r->token_stride : 0) + (long long)c->cfg.H * c->cfg.d) *
+           elt_size(c->cfg.dtype);
+}
+
+heads::Args common_args(const hla_heads* c, const int32_t* positions, int64_t pos_batch) {
+    heads::Args a{};
+    memcpy(a.turns, c->turns, sizeof(a.turns));
+    int stride = 1;
+    a.n_axes = c->rot ? c->cfg.n_axes : 0;
+    for (int i = 2; i >= 0; --i) {
+        a.pair_end[i] = c->pair_end[i];
+        a.grid[i] = c->grid_known && i < c->cfg.n_axes ? c->cfg.grid[i] : 1;
+        a.start[i] = c->cfg.start[i];
+        a.stride[i] = stride;
+        stride *= a.grid[i];
+    }
+    a.positions = positions;
+    a.pos_batch = pos_batch;
+    a.B = c->cfg.B; a.H = c->cfg.H; a.N = c->cfg.N; a.d = c->cfg.d;
+    a.log_lanes = c->log_lanes;
+    a.half = c->rot / 2;
+    a.rot_lanes = c->rot * elt_size(c->cfg.dtype) / 16;
+    a.eps = c->cfg.eps;
+    a.inv_d = 1.f / (float)c->cfg.d;
+    return a;
+}
+
+using Kernel = void (*)(heads::Args);
+
+template <template <typename, bool, bool> class K>
+Kernel pick(bool bf16, bool half, bool norm) {
+    if (bf16) return half ? (norm ? K<__nv_bfloat16, true, true>::get() : K<__nv_bfloat16, true, false>::get())
+                          : (norm ? K<__nv_bfloat16, false, true>::get() : K<__nv_bfloat16, false, false>::get());
+    return half ? (norm ? K<float, true, true>::get() : K<float, true, false>::get()) : (norm ? K<float, false, true>::get() : K<float, false, false>::get());
+}
+template <typename T, bool HALF, bool NORM> struct Fwd { static Kernel get() { return heads::forward_kernel<T, HALF, NORM>; } };
+template <typename T, bool HALF, bool NORM> struct Bwd { static Kernel get() { return heads::backward_kernel<T, HALF, NORM>; } };
+
+bool positions_ok(const hla_heads* c, const int32_t* positions, int64_t pos_batch) {
+    if (!c->rot) return true;
+    if (!positions) return c->grid_known;
+    if (reinterpret_cast<uintptr_t>(positions) & 3u) return false;
+    return pos_batch == 0 || (pos_batch >= (int64_t)c->cfg.N * c->cfg.n_axes && pos_batch < (1ll << 40));
+}
+
+bool weight_ok(const hla_heads* c, const void* w) { return !w || (c->cfg.norm && aligned16(w)); }
+
+}  // namespace
+
+extern "C" {
+
+hla_status hla_heads_create(const hla_heads_config* cfg, hla_heads** out) {
+    if (out) *out = nullptr;
+    if (!cfg || !out) return HLA_ERR_INVALID_ARG;
+    const hla_heads_config& c = *cfg;
+    if (c.B <= 0 || c.H <= 0 || c.N <= 0 || c.d <= 0) return HLA_ERR_INVALID_ARG;
+    if (c.dtype != HLA_BF16 && c.dtype != HLA_F32) return HLA_ERR_INVALID_ARG;
+    if (c.pairing != HLA_PAIR_ADJACENT && c.pairing != HLA_PAIR_HALVES) return HLA_ERR_INVALID_ARG;
+    if (c.norm != 0 && c.norm != 1) return HLA_ERR_INVALID_ARG;
+    if (c.n_axes < 0 || c.n_axes > 3) return HLA_ERR_INVALID_ARG;
+    if (!isfinite(c.q_scale) || !isfinite(c.theta) || c.theta < 0.0 || !isfinite(c.eps) || c.eps < 0.f) return HLA_ERR_INVALID_ARG;
+    int rot = 0;
+    long long tokens = 1;
+    bool any = false, all = true;
+    for (int i = 0; i < c.n_axes; ++i) {
+        if (c.axis_width[i] < 0 || (c.axis_width[i] & 1) || c.axis_width[i] > c.d || c.grid[i] < 0) return HLA_ERR_INVALID_ARG;
+        rot += c.axis_width[i];
+        any |= c.grid[i] > 0;
+        all &= c.grid[i] > 0;
+        if (c.grid[i] > 0 && tokens <= INT32_MAX) tokens *= c.grid[i];
+        if (c.start[i] > INT32_MAX - (c.grid[i] > 0 ? c.grid[i] : 0)) return HLA_ERR_INVALID_ARG;
+    }
+    if (rot > c.d) return HLA_ERR_INVALID_ARG;
+    if (any && (!all || tokens != c.N)) return HLA_ERR_INVALID_ARG;
+    for (int p = 0; c.inv_freq && p < rot / 2; ++p)
+        if (!isfinite(c.inv_freq[p])) return HLA_ERR_INVALID_ARG;
+    const int per = 16 / elt_size(c.dtype);
+    if (c.d > kMaxD || c.d % per) return HLA_ERR_UNSUPPORTED;                       // rows of whole 16-byte pieces
+    if (c.pairing == HLA_PAIR_HALVES && rot % per) return HLA_ERR_UNSUPPORTED;
+    if ((long long)c.B * c.H > 65535 || (long long)c.B * c.N > (1ll << 28)) return HLA_ERR_UNSUPPORTED;
+
+    hla_heads* x = new (std::nothrow) hla_heads();
+    if (!x) return HLA_ERR_NO_MEMORY;
+    x->cfg = c;
+    x->cfg.inv_freq = nullptr;
+    if (c.eps == 0.f) x->cfg.eps = 1e-6f;
+    if (c.q_scale == 0.f) x->cfg.q_scale = 1.f;
+    if (c.theta == 0.0) x->cfg.theta = 10000.0;
+    x->rot = rot;
+    x->grid_known = any;
+    for (int i = 0, pair = 0; i < 3; ++i) {
+        const int np = i < c.n_axes ? c.axis_width[i] / 2 : 0;
+        for (int j = 0; j < np; ++j, ++pair)
+            x->turns[pair] = (c.inv_freq ? c.inv_freq[pair] : pow(x->cfg.theta, -(double)j / np)) / 6.283185307179586476925287;
+        x->pair_end[i] = pair;
+    }
+    x->log_lanes = 0;
+    while ((per << x->log_lanes) < c.d) ++x->log_lanes;
+    x->sm_count = current_sm_count();
+    *out = x;
+    return HLA_OK;
+}
+
+size_t hla_heads_workspace_bytes(const hla_heads* c) {
+    if (!c || !c->cfg.norm) return 0;
+    // rows of partial sums: runs x blocks of the two normed tensors, whichever of the three are passed
+    size_t most = 0;
+    for (int tensors = 1; tensors <= 3; ++tensors) {
+        const int per = heads_per_run(c, tensors), chunks = (c->cfg.H + per - 1) / per;
+        const size_t rows = (size_t)(tensors < 2 ? tensors : 2) * chunks * backward_blocks(c, tensors * chunks);
+        if (rows > most) most = rows;
+    }
+    return (most * c->cfg.d * 4 + 255) / 256 * 256;
+}
+
+hla_status hla_heads_forward(hla_heads* c, const hla_rows* q, const hla_rows* k, const hla_rows* v, const void* wq, const void* wk,
+                             const int32_t* positions, int64_t positions_batch_stride, void* Q, void* K, void* V, void* cuda_stream) {
+    if (!c || (!q && !k && !v)) return HLA_ERR_INVALID_ARG;
+    const hla_rows* in[3] = {q, k, v};
+    void* to[3] = {Q, K, V};
+    const void* w[3] = {wq, wk, nullptr};
+    if (!weight_ok(c, wq) || !weight_ok(c, wk) || !positions_ok(c, positions, positions_batch_stride)) return HLA_ERR_INVALID_ARG;
+    const size_t dense = (size_t)c->cfg.B * c->cfg.H * c->cfg.N * c->cfg.d * elt_size(c->cfg.dtype);
+    heads::Args a = common_args(c, positions, positions_batch_stride);
+    const int elt = elt_size(c->cfg.dtype);
+    for (int i = 0; i < 3; ++i) {
+        if (!in[i] != !to[i]) return HLA_ERR_INVALID_ARG;
+        if (!in[i]) continue;
+        if (!rows_ok(c, in[i]) || !aligned16(to[i])) return HLA_ERR_INVALID_ARG;
+        for (int j = 0; j < 3; ++j) {      // an output over an input, or over another output
+            if (in[j] && in[j]->data && overlap(to[i], dense, in[j]->data, rows_span(c, in[j]))) return HLA_ERR_INVALID_ARG;
+            if (j != i && to[j] && overlap(to[i], dense, to[j], dense)) return HLA_ERR_INVALID_ARG;
+        }
+        heads::Tensor& t = a.t[a.n_tensors++];
+        t.x = static_cast<const char*>(in[i]->data);
+        t.x_batch = in[i]->batch_stride * elt;
+        t.x_token = in[i]->token_stride * elt;
+        t.out = static_cast<char*>(to[i]);
+        t.w = w[i];
+        t.scale = i == 0 ? c->cfg.q_scale : 1.f;
+        t.rotate = i < 2;
+    }
+    a.per_chunk = heads_per_run(c, a.n_tensors);
+    a.chunks = (a.H + a.per_chunk - 1) / a.per_chunk;
+    const uint32_t units = (uint32_t)a.B * a.N * a.n_tensors * a.chunks;
+    const int groups = heads::kThreads >> a.log_lanes;
+    const Kernel kern = pick<Fwd>(c->cfg.dtype == HLA_BF16, c->cfg.pairing == HLA_PAIR_HALVES, c->cfg.norm);
+    kern<<<(units + groups - 1) / groups, heads::kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
+    return cudaGetLastError() == cudaSuccess ? HLA_OK : HLA_ERR_CUDA;
+}
+
+hla_status hla_heads_backward(hla_heads* c, const void* dQ, const void* dK, const void* dV, const hla_rows* q, const hla_rows* k,
+                              const void* wq, const void* wk, const int32_t* positions, int64_t positions_batch_stride,
+                              const hla_rows_out* dq, const hla_rows_out* dk, const hla_rows_out* dv, void* dwq, void* dwk,
+                              void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!c || (!dQ && !dK && !dV)) return HLA_ERR_INVALID_ARG;
+    const void* dy[3] = {dQ, dK, dV};
+    const hla_rows* x[3] = {q, k, nullptr};
+    const hla_rows_out* to[3] = {dq, dk, dv};
+    const void* w[3] = {wq, wk, nullptr};
+    void* dw[2] = {dwq, dwk};
+    if (!weight_ok(c, wq) || !weight_ok(c, wk) || !positions_ok(c, positions, positions_batch_stride)) return HLA_ERR_INVALID_ARG;
+    const size_t dense = (size_t)c->cfg.B * c->cfg.H * c->cfg.N * c->cfg.d * elt_size(c->cfg.dtype);
+    heads::Args a = common_args(c, positions, positions_batch_stride);
+    const int elt = elt_size(c->cfg.dtype);
+    float* sums[2] = {nullptr, nullptr};
+    int normed = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (!dy[i] != !to[i]) return HLA_ERR_INVALID_ARG;
+        if (i < 2 && dw[i] && (!c->cfg.norm || !dy[i] || (reinterpret_cast<uintptr_t>(dw[i]) & 3u))) return HLA_ERR_INVALID_ARG;
+        if (!dy[i]) continue;
+        const bool needs_x = i < 2 && c->cfg.norm;
+        const hla_rows o = {to[i]->data, to[i]->batch_stride, to[i]->token_stride};
+        if (!aligned16(dy[i]) || !rows_ok(c, &o)) return HLA_ERR_INVALID_ARG;
+        if (needs_x && (!x[i] || !rows_ok(c, x[i]))) return HLA_ERR_INVALID_ARG;
+        for (int j = 0; j < 3; ++j) {
+            if (dy[j] && overlap(o.data, rows_span(c, &o), dy[j], dense)) return HLA_ERR_INVALID_ARG;
+            if (j < 2 && c->cfg.norm && x[j] && x[j]->data && dy[j] && overlap(o.data, rows_span(c, &o), x[j]->data, rows_span(c, x[j]))) return HLA_ERR_INVALID_ARG;
+        }
+        heads::Tensor& t = a.t[a.n_tensors++];
+        t.dy = static_cast<const char*>(dy[i]);
+        t.out = static_cast<char*>(to[i]->data);
+        t.o_batch = o.batch_stride * elt;
+        t.o_token = o.token_stride * elt;
+        if (needs_x) {
+            t.x = static_cast<const char*>(x[i]->data);
+            t.x_batch = x[i]->batch_stride * elt;
+            t.x_token = x[i]->token_stride * elt;
+            sums[normed++] = static_cast<float*>(dw[i]);
+        }
+        t.w = w[i];
+        t.scale = i == 0 ? c->cfg.q_scale : 1.f;
+        t.rotate = i < 2;
+    }
+    a.want_dw = sums[0] || sums[1];
+    if (a.want_dw) {
+        if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
+        if (workspace_bytes < hla_heads_workspace_bytes(c)) return HLA_ERR_WORKSPACE;
+        a.part = static_cast<float*>(workspace);
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    a.per_chunk = heads_per_run(c, a.n_tensors);
+    a.chunks = (a.H + a.per_chunk - 1) / a.per_chunk;
+    const int blocks = backward_blocks(c, a.n_tensors * a.chunks);
+    const Kernel kern = pick<Bwd>(c->cfg.dtype == HLA_BF16, c->cfg.pairing == HLA_PAIR_HALVES, c->cfg.norm);
+    kern<<<dim3(blocks, a.n_tensors * a.chunks), heads::kThreads, 0, st>>>(a);
+    if (cudaGetLastError() != cudaSuccess) return HLA_ERR_CUDA;
+    if (a.want_dw && !launch_behind(heads::dw_kernel, dim3((a.d + 31) / 32, normed), heads::kDwThreads, st, (const float*)a.part, a.chunks * blocks, a.d, sums[0], sums[1]))
+        return HLA_ERR_CUDA;
+    return HLA_OK;
+}
+
+hla_status hla_heads_destroy(hla_heads* c) {
+    if (!c) return HLA_ERR_INVALID_ARG;
+    delete c;
+    return HLA_OK;
+}
+
+}  // extern "C"
