@@ -17,6 +17,7 @@
 #include <new>
 
 #include "hla_ops_common.cuh"
+#include "hla_tc_prim.cuh"
 
 namespace hla {
 namespace scan {
@@ -24,8 +25,8 @@ namespace scan {
 constexpr int kThreads = 256;
 constexpr int kLanes = 16;                       // threads side by side on channels, two each
 constexpr int kRuns = kThreads / kLanes;
-constexpr int kRun = 8;                          // tokens of a thread
-constexpr int kPiece = kRuns * kRun;             // tokens of a block between two exchanges
+template <typename T> constexpr int kRunOf = sizeof(T) == 2 ? 8 : 4;            // tokens of a thread: as many as its registers hold
+template <typename T> constexpr int kPieceOf = kRuns * kRunOf<T>;               // tokens of a block between two exchanges
 constexpr int kTile = 2 * kLanes;                // channels of a block
 constexpr int kMaxCluster = 8;
 
@@ -33,7 +34,6 @@ enum { kLog = 0, kSigmoid = 1 };
 
 struct Args {
     int N, C, pieces;                            // pieces: exchanges of a block
-    int vec;                                     // two channels can be moved as one word
     const char *x, *g, *h, *dh;
     char *out0, *out1;                           // forward: h, -; backward: dx, dg
     long long x_batch, x_token, g_batch, g_token;      // elements
@@ -44,224 +44,349 @@ struct Args {
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ uint32_t cluster_blocks() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ void store_remote(float4* local, uint32_t rank, const float4& v) {
-    uint32_t a = (uint32_t)__cvta_generic_to_shared(local), r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(r), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t of_block(uint32_t local, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(rank));
+    return r;
 }
 
-// Two neighbouring channels of one token, as they are in memory.
-template <typename T> struct Two;
-template <> struct Two<__nv_bfloat16> {
+// ---- two channels in one register pair -------------------------------------------------------------------------------------
+using P2 = unsigned long long;
+__device__ __forceinline__ P2 pair(float x, float y) { P2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y)); return r; }
+__device__ __forceinline__ float2 both(P2 v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ P2 fma2(P2 a, P2 b, P2 c) { P2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ P2 mul2(P2 a, P2 b) { P2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ P2 add2(P2 a, P2 b) { P2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ P2 twice(float x) { return pair(x, x); }
+__device__ __forceinline__ P2 one_minus(P2 x) { return fma2(x, twice(-1.f), twice(1.f)); }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Two neighbouring channels of one token, as they are in memory.  VEC: they are one aligned word; else one by one, and `second` says
+// whether the second channel exists.
+template <typename T, bool VEC> struct Two;
+template <bool VEC> struct Two<__nv_bfloat16, VEC> {
     using Raw = uint32_t;
     static __device__ __forceinline__ Raw none() { return 0; }
-    static __device__ __forceinline__ Raw load(const char* base, long long i, bool vec, bool second) {
-        const unsigned short* p = reinterpret_cast<const unsigned short*>(base) + i;
-        if (vec) return *reinterpret_cast<const uint32_t*>(p);
+    static __device__ __forceinline__ Raw load(const char* at, bool second) {
+        if (VEC) return __ldg(reinterpret_cast<const uint32_t*>(at));
+        const unsigned short* p = reinterpret_cast<const unsigned short*>(at);
         return p[0] | (second ? (uint32_t)p[1] << 16 : 0u);
     }
-    static __device__ __forceinline__ float2 get(Raw r) { return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u)); }
-    static __device__ __forceinline__ void store(char* base, long long i, bool vec, bool second, float2 v) {
-        __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(base) + i;
-        if (vec) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(v.x, v.y); return; }
-        p[0] = __float2bfloat16_rn(v.x);
-        if (second) p[1] = __float2bfloat16_rn(v.y);
+    static __device__ __forceinline__ P2 get(Raw r) { return pair(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u)); }
+    static __device__ __forceinline__ void store(char* at, bool second, P2 v) {
+        const float2 f = both(v);
+        __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(at);
+        if (VEC) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(f.x, f.y); return; }
+        p[0] = __float2bfloat16_rn(f.x);
+        if (second) p[1] = __float2bfloat16_rn(f.y);
     }
 };
-template <> struct Two<float> {
-    using Raw = float2;
-    static __device__ __forceinline__ Raw none() { return make_float2(0.f, 0.f); }
-    static __device__ __forceinline__ Raw load(const char* base, long long i, bool vec, bool second) {
-        const float* p = reinterpret_cast<const float*>(base) + i;
-        if (vec) return *reinterpret_cast<const float2*>(p);
-        return make_float2(p[0], second ? p[1] : 0.f);
+template <bool VEC> struct Two<float, VEC> {
+    using Raw = P2;
+    static __device__ __forceinline__ Raw none() { return 0; }
+    static __device__ __forceinline__ Raw load(const char* at, bool second) {
+        if (VEC) return __ldg(reinterpret_cast<const unsigned long long*>(at));
+        const float* p = reinterpret_cast<const float*>(at);
+        return pair(p[0], second ? p[1] : 0.f);
     }
-    static __device__ __forceinline__ float2 get(Raw r) { return r; }
-    static __device__ __forceinline__ void store(char* base, long long i, bool vec, bool second, float2 v) {
-        float* p = reinterpret_cast<float*>(base) + i;
-        if (vec) { *reinterpret_cast<float2*>(p) = v; return; }
-        p[0] = v.x;
-        if (second) p[1] = v.y;
+    static __device__ __forceinline__ P2 get(Raw r) { return r; }
+    static __device__ __forceinline__ void store(char* at, bool second, P2 v) {
+        if (VEC) { *reinterpret_cast<P2*>(at) = v; return; }
+        const float2 f = both(v);
+        float* p = reinterpret_cast<float*>(at);
+        p[0] = f.x;
+        if (second) p[1] = f.y;
     }
 };
+// fp32 values of a state [B][C].
+__device__ __forceinline__ P2 load_state(const float* p, size_t i, bool live, bool second) {
+    return p && live ? pair(p[i], second ? p[i + 1] : 0.f) : 0;
+}
+__device__ __forceinline__ void store_state(float* p, size_t i, bool second, P2 v) {
+    const float2 f = both(v);
+    p[i] = f.x;
+    if (second) p[i + 1] = f.y;
+}
 
-// a and 1 - a.  Where the memory is long a is near 1, and an error of a relative 2^-22 of every a would add up over it: expf, not the
-// fast form; and 1 - a is formed without the difference.
-template <int GATE, bool REST>
-__device__ __forceinline__ void gate1(float g, float& a, float& rest) {
+// a and 1 - a.  Where the memory is long a is near 1, and an error of a relative 2^-22 of every a would add up over it; so the smaller of
+// the two is formed first, with an error of its own size, and the larger is its difference to 1, correctly rounded.
+template <int GATE>
+__device__ __forceinline__ void gate(P2 g, P2& a, P2& rest) {
     if (GATE == kLog) {
-        a = expf(g);
-        if (REST) rest = -expm1f(g);
+        // 1 - exp(g) = -g (1 + g/2 (1 + g/3 (1 + ...))): six terms leave 5e-8 of it up to 1/4; beyond, a memory is at most four tokens
+        P2 p = fma2(g, twice(1.f / 720), twice(1.f / 120));
+        p = fma2(g, p, twice(1.f / 24));
+        p = fma2(g, p, twice(1.f / 6));
+        p = fma2(g, p, twice(0.5f));
+        p = fma2(g, p, twice(1.f));
+        const float2 x = both(g), near = both(mul2(mul2(g, twice(-1.f)), p)), t = both(mul2(g, twice(1.4426950408889634f)));
+        const float2 e = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+        const bool nx = fabsf(x.x) < 0.25f, ny = fabsf(x.y) < 0.25f;
+        rest = pair(nx ? near.x : 1.f - e.x, ny ? near.y : 1.f - e.y);
+        a = pair(nx ? 1.f - near.x : e.x, ny ? 1.f - near.y : e.y);
     } else {
-        const float e = expf(-fabsf(g)), r = 1.f / (1.f + e), s = e * r;      // the larger and the smaller of the two
-        a = g >= 0.f ? r : s;
-        if (REST) rest = g >= 0.f ? s : r;
+        // r = 1 / (1 + exp(-g)): the smaller of the two is e r or r, the larger its difference to 1
+        const float2 x = both(g), t = both(mul2(g, twice(-1.4426950408889634f)));
+        const P2 e = pair(exp2_fast(t.x), exp2_fast(t.y));
+        const float2 d = both(add2(e, twice(1.f)));
+        const P2 r = pair(reciprocal(d.x), reciprocal(d.y));
+        const bool px = x.x >= 0.f, py = x.y >= 0.f;
+        const float2 er = both(mul2(e, r)), rr = both(r);
+        const P2 small = pair(px ? er.x : rr.x, py ? er.y : rr.y);
+        const float2 v = both(small), w = both(one_minus(small));
+        a = pair(px ? w.x : v.x, py ? w.y : v.y);
+        rest = pair(px ? v.x : w.x, py ? v.y : w.y);
     }
 }
-template <int GATE, bool REST>
-__device__ __forceinline__ void gate(float2 g, float2& a, float2& rest) {
-    gate1<GATE, REST>(g.x, a.x, rest.x);
-    gate1<GATE, REST>(g.y, a.y, rest.y);
-}
-
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return make_float2(a.x * b.x, a.y * b.y); }
 
 struct Exchange {
-    float4 runs[kRuns][kLanes];                          // maps (A, A, H, H) of this block's runs
-    float4 blocks[2][kMaxCluster][kLanes];               // of the cluster's blocks, of this piece and the next
+    ulonglong2 warps[kRuns / 2][kLanes];                 // maps (A, H) of this block's warps, two runs each
+    ulonglong2 blocks[2][kMaxCluster][kLanes];           // of the cluster's blocks, of this piece and the next
+    uint64_t full[2];                                    // barriers: the maps of all blocks are there
 };
 
-// From the map (A, H) of this thread's run: the state before its first token; `carry`, the state before the cluster's piece, becomes
-// the one behind it.  Every thread of the cluster calls this once a piece.
-__device__ __forceinline__ float2 state_before(Exchange& e, float2 A, float2 H, float2& carry, int parity, int lane, int run, int rank, int blocks) {
-    e.runs[run][lane] = make_float4(A.x, A.y, H.x, H.y);
-    __syncthreads();
-    float2 PA = make_float2(1.f, 1.f), PH = make_float2(0.f, 0.f);
-    for (int r = 0; r < run; ++r) {
-        const float4 q = e.runs[r][lane];
-        const float2 qa = make_float2(q.x, q.y);
-        PH = fma2(qa, PH, make_float2(q.z, q.w));
-        PA = mul2(qa, PA);
-    }
-    if (run == kRuns - 1) {
-        const float2 TA = mul2(A, PA), TH = fma2(A, PH, H);
-        for (int i = 0; i < blocks; ++i) store_remote(&e.blocks[parity][rank][lane], i, make_float4(TA.x, TA.y, TH.x, TH.y));
-    }
-    cluster_arrive();
-    cluster_wait();
-    float2 mine = carry;
-    for (int i = 0; i < blocks; ++i) {
-        if (i == rank) mine = carry;
-        const float4 q = e.blocks[parity][i][lane];
-        carry = fma2(make_float2(q.x, q.y), carry, make_float2(q.z, q.w));
-    }
-    return fma2(PA, mine, PH);
-}
+// Every map of a piece is written by its block straight into the shared memory of all blocks of the cluster and counted by their barriers.
+// A buffer is written again two pieces later: by then its writer has had this block's map of the piece between, which this block sends
+// behind its reads of the buffer.
+struct Cluster {
+    Exchange& e;
+    int lane, run, rank, blocks;
+    bool lost;
 
-template <typename T, int GATE, bool CONVEX>
-__global__ void __launch_bounds__(kThreads) forward_kernel(const __grid_constant__ Args p) {
-    using V = Two<T>;
-    __shared__ Exchange e;
-    const int lane = threadIdx.x % kLanes, run = threadIdx.x / kLanes, rank = cluster_rank(), blocks = cluster_blocks();
-    const int c = blockIdx.y * kTile + 2 * lane, b = blockIdx.z;
-    const bool live = c < p.C, second = c + 1 < p.C;
-    const long long xo = b * p.x_batch + c, go = b * p.g_batch + c, oo = (long long)b * p.N * p.C + c;
-    float2 carry = make_float2(0.f, 0.f);
-    if (p.in && live) {
-        carry.x = p.in[(size_t)b * p.C + c];
-        if (second) carry.y = p.in[(size_t)b * p.C + c + 1];
+    __device__ __forceinline__ Cluster(Exchange& x) : e(x), lane(threadIdx.x % kLanes), run(threadIdx.x / kLanes), rank(cluster_rank()), blocks(cluster_blocks()), lost(false) {}
+    __device__ __forceinline__ void start() {
+        if (threadIdx.x == 0) {
+            tc::mbar_init(&e.full[0], 1);
+            tc::mbar_init(&e.full[1], 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        cluster_sync();
     }
-    typename V::Raw rg[kRun], rx[kRun];
-    auto fetch = [&](int t0) {
+    // From the map (A, H) of this thread's run: the state before its first token; `carry`, the state before the cluster's piece, becomes
+    // the one behind it.  Every thread of the cluster calls this once a piece.
+    __device__ __forceinline__ P2 state_before(P2 A, P2 H, P2& carry, int piece) {
+        const int buffer = piece & 1, warp = run >> 1;
+        const bool second = run & 1;
+        // the other run of the warp; the second run's thread forms the map of both
+        const P2 qa = __shfl_xor_sync(0xffffffffu, A, kLanes), qh = __shfl_xor_sync(0xffffffffu, H, kLanes);
+        const P2 WA = mul2(A, qa), WH = fma2(A, qh, H);
+        if (threadIdx.x == 0) tc::mbar_arrive_expect_tx(&e.full[buffer], blocks * kLanes * (int)sizeof(ulonglong2));
+        if (second) e.warps[warp][lane] = make_ulonglong2(WA, WH);
+        __syncthreads();
+        P2 PA = twice(1.f), PH = 0;
 #pragma unroll
-        for (int k = 0; k < kRun; ++k) {
-            rg[k] = rx[k] = V::none();
-            if (live && t0 + k < p.N) {
-                rg[k] = V::load(p.g, go + (long long)(t0 + k) * p.g_token, p.vec, second);
-                rx[k] = V::load(p.x, xo + (long long)(t0 + k) * p.x_token, p.vec, second);
+        for (int w = 0; w < kRuns / 2 - 1; ++w) {
+            if (w >= warp) break;
+            const ulonglong2 q = e.warps[w][lane];
+            PH = fma2(q.x, PH, q.y);
+            PA = mul2(q.x, PA);
+        }
+        if (run == kRuns - 1) {
+            const float2 ta = both(mul2(WA, PA)), th = both(fma2(WA, PH, WH));
+            const uint32_t to = tc::smem_u32(&e.blocks[buffer][rank][lane]), bar = tc::smem_u32(&e.full[buffer]);
+            for (int i = 0; i < blocks; ++i)
+                asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(of_block(to, i)), "f"(ta.x), "f"(ta.y), "f"(th.x),
+                             "f"(th.y), "r"(of_block(bar, i))
+                             : "memory");
+        }
+        if (second) {
+            PH = fma2(qa, PH, qh);
+            PA = mul2(qa, PA);
+        }
+        if (!lost && !tc::mbar_wait(&e.full[buffer], (piece >> 1) & 1)) {      // (two seconds: the outputs from here on are not numbers)
+            lost = true;
+            carry = twice(__int_as_float(0x7fc00000));
+        }
+        P2 mine = carry;
+        for (int i = 0; i < blocks; ++i) {
+            if (i == rank) mine = carry;
+            const ulonglong2 q = e.blocks[buffer][i][lane];
+            carry = fma2(q.x, carry, q.y);
+        }
+        return fma2(PA, mine, PH);
+    }
+};
+
+template <typename T, int GATE, bool CONVEX, bool VEC>
+__global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_constant__ Args p) {
+    using V = Two<T, VEC>;
+    constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>;
+    __shared__ Exchange e;
+    Cluster cl(e);
+    const int c = blockIdx.y * kTile + 2 * cl.lane, b = blockIdx.z;
+    const bool live = c < p.C, second = c + 1 < p.C;
+    const size_t at_state = (size_t)b * p.C + c;
+    P2 carry = load_state(p.in, at_state, live, second);
+    const long long gs = p.g_token * (int)sizeof(T), xs = p.x_token * (int)sizeof(T), os = (long long)p.C * (int)sizeof(T);
+    int t0 = cl.rank * kPiece + cl.run * kRun;
+    const int stride = cl.blocks * kPiece;
+    const char* pg = p.g + (b * p.g_batch + c) * (int)sizeof(T) + t0 * gs;
+    const char* px = p.x + (b * p.x_batch + c) * (int)sizeof(T) + t0 * xs;
+    char* po = p.out0 + ((long long)b * p.N * p.C + c) * (int)sizeof(T) + t0 * os;
+    typename V::Raw rg[kRun], rx[kRun];
+    auto fetch = [&](int t) {
+        if (live && t + kRun <= p.N) {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                rg[k] = V::load(pg + k * gs, second);
+                rx[k] = V::load(px + k * xs, second);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                const bool in = live && t + k < p.N;
+                rg[k] = in ? V::load(pg + k * gs, second) : V::none();
+                rx[k] = in ? V::load(px + k * xs, second) : V::none();
             }
         }
+        pg += stride * gs;
+        px += stride * xs;
     };
-    int t0 = rank * kPiece + run * kRun;
     fetch(t0);
+    cl.start();
     for (int s = 0; s < p.pieces; ++s) {
-        float2 a[kRun], u[kRun], A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
+        P2 a[kRun], u[kRun];
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
-            float2 rest;
-            gate<GATE, CONVEX>(V::get(rg[k]), a[k], rest);
+            P2 rest;
+            gate<GATE>(V::get(rg[k]), a[k], rest);
             u[k] = V::get(rx[k]);
             if (CONVEX) u[k] = mul2(rest, u[k]);
-            if (t0 + k >= p.N) { a[k] = make_float2(1.f, 1.f); u[k] = make_float2(0.f, 0.f); }      // behind the end nothing changes
+        }
+        const bool whole = live && t0 + kRun <= p.N;
+        if (!whole) {      // behind the end nothing changes
+#pragma unroll
+            for (int k = 0; k < kRun; ++k)
+                if (t0 + k >= p.N) { a[k] = twice(1.f); u[k] = 0; }
+        }
+        P2 A = a[0], H = u[0];
+#pragma unroll
+        for (int k = 1; k < kRun; ++k) {
             H = fma2(a[k], H, u[k]);
             A = mul2(a[k], A);
         }
-        const int next = t0 + blocks * kPiece;
-        if (s + 1 < p.pieces) fetch(next);
-        float2 h = state_before(e, A, H, carry, s & 1, lane, run, rank, blocks);
+        if (s + 1 < p.pieces) fetch(t0 + stride);
+        P2 h = cl.state_before(A, H, carry, s);
+        if (whole) {
 #pragma unroll
-        for (int k = 0; k < kRun; ++k) {
-            h = fma2(a[k], h, u[k]);
-            if (live && t0 + k < p.N) V::store(p.out0, oo + (long long)(t0 + k) * p.C, p.vec, second, h);
+            for (int k = 0; k < kRun; ++k) {
+                h = fma2(a[k], h, u[k]);
+                V::store(po + k * os, second, h);
+            }
+        } else if (live) {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                h = fma2(a[k], h, u[k]);
+                if (t0 + k < p.N) V::store(po + k * os, second, h);
+            }
         }
-        t0 = next;
+        po += stride * os;
+        t0 += stride;
     }
-    if (p.last && rank == 0 && run == 0 && live) {
-        p.last[(size_t)b * p.C + c] = carry.x;
-        if (second) p.last[(size_t)b * p.C + c + 1] = carry.y;
-    }
+    if (p.last && cl.rank == 0 && cl.run == 0 && live) store_state(p.last, at_state, second, carry);
+    cluster_sync();      // no block leaves while another may still write into its shared memory
 }
 
-// Tokens are counted from the end: i = N - 1 - t.
-template <typename T, int GATE, bool CONVEX>
-__global__ void __launch_bounds__(kThreads) backward_kernel(const __grid_constant__ Args p) {
-    using V = Two<T>;
+// Tokens are counted from the end: i = N - 1 - t; pointers go down.
+template <typename T, int GATE, bool CONVEX, bool VEC>
+__global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Args p) {
+    using V = Two<T, VEC>;
     using Raw = typename V::Raw;
+    constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>;
     __shared__ Exchange e;
-    const int lane = threadIdx.x % kLanes, run = threadIdx.x / kLanes, rank = cluster_rank(), blocks = cluster_blocks();
-    const int c = blockIdx.y * kTile + 2 * lane, b = blockIdx.z;
+    Cluster cl(e);
+    const int c = blockIdx.y * kTile + 2 * cl.lane, b = blockIdx.z;
     const bool live = c < p.C, second = c + 1 < p.C;
-    const long long xo = b * p.x_batch + c, go = b * p.g_batch + c, oo = (long long)b * p.N * p.C + c;
-    float2 carry = make_float2(0.f, 0.f), h0 = make_float2(0.f, 0.f);
-    if (live) {
-        const size_t at = (size_t)b * p.C + c;
-        if (p.in) { carry.x = p.in[at]; if (second) carry.y = p.in[at + 1]; }
-        if (p.h0) { h0.x = p.h0[at]; if (second) h0.y = p.h0[at + 1]; }
-    }
-    Raw rg[kRun], rd[kRun], rh[kRun], rx[kRun];
-    auto fetch = [&](int i0) {
+    const size_t at_state = (size_t)b * p.C + c;
+    P2 carry = load_state(p.in, at_state, live, second);
+    const P2 h0 = load_state(p.h0, at_state, live, second);
+    const long long gs = p.g_token * (int)sizeof(T), xs = p.x_token * (int)sizeof(T), os = (long long)p.C * (int)sizeof(T);
+    int i0 = cl.rank * kPiece + cl.run * kRun;
+    const int stride = cl.blocks * kPiece;
+    const long long t_first = p.N - 1 - i0;
+    const char* pg = p.g + (b * p.g_batch + c) * (int)sizeof(T) + t_first * gs;
+    const char* px = CONVEX ? p.x + (b * p.x_batch + c) * (int)sizeof(T) + t_first * xs : nullptr;
+    const long long dense = ((long long)b * p.N * p.C + c) * (int)sizeof(T) + t_first * os;
+    const char *pd = p.dh + dense, *ph = p.h + dense - os;
+    char *po0 = p.out0 + dense, *po1 = p.out1 + dense;
+    Raw rg[kRun], rd[kRun];
+    auto fetch = [&](int i) {
+        if (live && i + kRun <= p.N) {
 #pragma unroll
-        for (int k = 0; k < kRun; ++k) {
-            const int t = p.N - 1 - (i0 + k);
-            rg[k] = rd[k] = rh[k] = rx[k] = V::none();
-            if (live && t >= 0) {
-                rg[k] = V::load(p.g, go + (long long)t * p.g_token, p.vec, second);
-                rd[k] = V::load(p.dh, oo + (long long)t * p.C, p.vec, second);
-                if (t > 0) rh[k] = V::load(p.h, oo + (long long)(t - 1) * p.C, p.vec, second);
-                if (CONVEX) rx[k] = V::load(p.x, xo + (long long)t * p.x_token, p.vec, second);
+            for (int k = 0; k < kRun; ++k) {
+                rg[k] = V::load(pg - k * gs, second);
+                rd[k] = V::load(pd - k * os, second);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                const bool in = live && i + k < p.N;
+                rg[k] = in ? V::load(pg - k * gs, second) : V::none();
+                rd[k] = in ? V::load(pd - k * os, second) : V::none();
             }
         }
+        pg -= stride * gs;
+        pd -= stride * os;
     };
-    int i0 = rank * kPiece + run * kRun;
     fetch(i0);
+    cl.start();
     for (int s = 0; s < p.pieces; ++s) {
-        constexpr bool REST = CONVEX || GATE == kSigmoid;
-        float2 a[kRun], rest[kRun], d[kRun], w[kRun], A = make_float2(1.f, 1.f), M = make_float2(0.f, 0.f);
+        // what only the second going-through needs is on its way during the exchange
+        Raw rh[kRun], rx[kRun], now[kRun];
+        const bool whole = live && i0 + kRun < p.N;      // (the state before token 0 is h0)
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
-            gate<GATE, REST>(V::get(rg[k]), a[k], rest[k]);
-            d[k] = V::get(rd[k]);
-            w[k] = i0 + k == p.N - 1 ? h0 : V::get(rh[k]);
-            if (CONVEX) { const float2 x = V::get(rx[k]); w[k].x -= x.x; w[k].y -= x.y; }
-            if (i0 + k >= p.N) { a[k] = make_float2(1.f, 1.f); d[k] = make_float2(0.f, 0.f); }
-            M = mul2(a[k], make_float2(d[k].x + M.x, d[k].y + M.y));
-            A = mul2(a[k], A);
+            rh[k] = whole || (live && i0 + k + 1 < p.N) ? V::load(ph - k * os, second) : V::none();
+            rx[k] = CONVEX && (whole || (live && i0 + k < p.N)) ? V::load(px - k * xs, second) : V::none();
         }
-        const int next = i0 + blocks * kPiece;
-        if (s + 1 < p.pieces) fetch(next);
-        float2 mu = state_before(e, A, M, carry, s & 1, lane, run, rank, blocks);
+        P2 a[kRun], rest[kRun], A, M;
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
-            const float2 lam = make_float2(d[k].x + mu.x, d[k].y + mu.y);
+            now[k] = rd[k];
+            gate<GATE>(V::get(rg[k]), a[k], rest[k]);
+            if (!whole && i0 + k >= p.N) a[k] = twice(1.f);      // (its dh was not read and is zero)
+            const P2 d = V::get(now[k]);
+            M = mul2(a[k], k ? add2(d, M) : d);
+            A = k ? mul2(a[k], A) : a[k];
+        }
+        if (s + 1 < p.pieces) fetch(i0 + stride);
+        P2 mu = cl.state_before(A, M, carry, s);
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+            const P2 lam = add2(V::get(now[k]), mu);
             mu = mul2(a[k], lam);
-            float2 dg = mul2(mu, w[k]);      // lambda a (h_{t-1} - x)
+            P2 w = !whole && i0 + k == p.N - 1 ? h0 : V::get(rh[k]);
+            if (CONVEX) w = fma2(V::get(rx[k]), twice(-1.f), w);
+            P2 dg = mul2(mu, w);      // lambda a (h_{t-1} - x)
             if (GATE == kSigmoid) dg = mul2(dg, rest[k]);
-            const float2 dx = CONVEX ? mul2(lam, rest[k]) : lam;
-            const int t = p.N - 1 - (i0 + k);
-            if (live && t >= 0) {
-                V::store(p.out0, oo + (long long)t * p.C, p.vec, second, dx);
-                V::store(p.out1, oo + (long long)t * p.C, p.vec, second, dg);
+            const P2 dx = CONVEX ? mul2(lam, rest[k]) : lam;
+            if (whole || (live && i0 + k < p.N)) {
+                V::store(po0 - k * os, second, dx);
+                V::store(po1 - k * os, second, dg);
             }
         }
-        i0 = next;
+        ph -= stride * os;
+        px -= CONVEX ? stride * xs : 0;
+        po0 -= stride * os;
+        po1 -= stride * os;
+        i0 += stride;
     }
-    if (p.last && rank == 0 && run == 0 && live) {
-        p.last[(size_t)b * p.C + c] = carry.x;
-        if (second) p.last[(size_t)b * p.C + c + 1] = carry.y;
-    }
+    if (p.last && cl.rank == 0 && cl.run == 0 && live) store_state(p.last, at_state, second, carry);
+    cluster_sync();
 }
 
 }  // namespace scan
@@ -278,17 +403,19 @@ namespace {
 
 using Kernel = void (*)(scan::Args);
 
-template <template <typename, int, bool> class K, typename T>
+template <template <typename, int, bool, bool> class K, typename T, bool VEC>
 Kernel pick_of(bool sigmoid, bool convex) {
-    if (sigmoid) return convex ? K<T, scan::kSigmoid, true>::get() : K<T, scan::kSigmoid, false>::get();
-    return convex ? K<T, scan::kLog, true>::get() : K<T, scan::kLog, false>::get();
+    if (sigmoid) return convex ? K<T, scan::kSigmoid, true, VEC>::get() : K<T, scan::kSigmoid, false, VEC>::get();
+    return convex ? K<T, scan::kLog, true, VEC>::get() : K<T, scan::kLog, false, VEC>::get();
 }
-template <template <typename, int, bool> class K>
-Kernel pick(const hla_scan_config& c) {
-    return c.dtype == HLA_BF16 ? pick_of<K, __nv_bfloat16>(c.gate == HLA_GATE_SIGMOID, c.convex) : pick_of<K, float>(c.gate == HLA_GATE_SIGMOID, c.convex);
+template <template <typename, int, bool, bool> class K>
+Kernel pick(const hla_scan_config& c, bool vec) {
+    const bool s = c.gate == HLA_GATE_SIGMOID, v = c.convex;
+    if (c.dtype == HLA_BF16) return vec ? pick_of<K, __nv_bfloat16, true>(s, v) : pick_of<K, __nv_bfloat16, false>(s, v);
+    return vec ? pick_of<K, float, true>(s, v) : pick_of<K, float, false>(s, v);
 }
-template <typename T, int GATE, bool CONVEX> struct Fwd { static Kernel get() { return scan::forward_kernel<T, GATE, CONVEX>; } };
-template <typename T, int GATE, bool CONVEX> struct Bwd { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX>; } };
+template <typename T, int GATE, bool CONVEX, bool VEC> struct Fwd { static Kernel get() { return scan::forward_kernel<T, GATE, CONVEX, VEC>; } };
+template <typename T, int GATE, bool CONVEX, bool VEC> struct Bwd { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX, VEC>; } };
 
 int elt_size(int dtype) { return dtype == HLA_BF16 ? 2 : 4; }
 
@@ -305,16 +432,16 @@ scan::Args common_args(const hla_scan* c) {
 }
 
 // Whether two channels lie in one aligned word everywhere.
-int vectors(const hla_scan* c, const scan::Args& a) {
+bool vectors(const hla_scan* c, const scan::Args& a) {
     const uintptr_t word = 2 * elt_size(c->cfg.dtype), at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.g);
     return !((a.C | a.x_batch | a.x_token | a.g_batch | a.g_token) & 1) && at % word == 0;
 }
 
 hla_status launch(const hla_scan* c, Kernel kern, scan::Args& a, cudaStream_t st) {
-    a.vec = vectors(c, a);
     int blocks = 1;      // of a cluster
-    while (blocks < scan::kMaxCluster && blocks * scan::kPiece < a.N) blocks *= 2;
-    a.pieces = (int)((a.N + (long long)blocks * scan::kPiece - 1) / (blocks * scan::kPiece));
+    const int piece = c->cfg.dtype == HLA_BF16 ? scan::kPieceOf<__nv_bfloat16> : scan::kPieceOf<float>;
+    while (blocks < scan::kMaxCluster && blocks * piece < a.N) blocks *= 2;
+    a.pieces = (int)((a.N + (long long)blocks * piece - 1) / (blocks * piece));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks, (a.C + scan::kTile - 1) / scan::kTile, c->cfg.B);
     cfg.blockDim = dim3(scan::kThreads);
@@ -372,7 +499,7 @@ hla_status hla_scan_forward(hla_scan* c, const void* x, const void* g, const voi
     a.out0 = static_cast<char*>(h);
     a.in = static_cast<const float*>(h0);
     a.last = static_cast<float*>(h_last);
-    return launch(c, pick<Fwd>(c->cfg), a, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, pick<Fwd>(c->cfg, vectors(c, a)), a, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const void* h0, const void* h, const void* dh, const void* dh_last,
@@ -408,7 +535,7 @@ hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const vo
     a.in = static_cast<const float*>(dh_last);
     a.h0 = static_cast<const float*>(h0);
     a.last = static_cast<float*>(dh0);
-    return launch(c, pick<Bwd>(c->cfg), a, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, pick<Bwd>(c->cfg, vectors(c, a)), a, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_destroy(hla_scan* c) {

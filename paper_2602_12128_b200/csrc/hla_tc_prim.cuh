@@ -103,7 +103,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, unsign
 }
 // The same wait with its polling loop out of line: a kernel with many wait sites and many warp roles keeps its
 // instruction footprint (and with it the misses of the per-SM instruction cache) small this way.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar_addr, uint32_t parity) {
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar_addr, uint32_t parity) {
     const unsigned long long t0 = global_timer_ns();
     for (;;) {
         uint32_t ok;
