@@ -75,19 +75,13 @@ __device__ __forceinline__ float reciprocal(float x) {
     return r;
 }
 
-// Two neighbouring channels of one token, as they are in memory.  VEC: they are one aligned word; else one by one, and `second` says
-// whether the second channel exists.
-template <typename T, bool VEC> struct Two;
-template <bool VEC> struct Two<__nv_bfloat16, VEC> {
+// Two neighbouring channels of one token.  VEC: they are one aligned word of the outputs; else they go one by one, and `second` says whether
+// the second channel exists.
+template <typename T> struct Two;
+template <> struct Two<__nv_bfloat16> {
     using Raw = uint32_t;
-    static __device__ __forceinline__ Raw none() { return 0; }
-    static __device__ __forceinline__ Raw load(const char* at, bool second) {
-        if (VEC) return __ldg(reinterpret_cast<const uint32_t*>(at));
-        const unsigned short* p = reinterpret_cast<const unsigned short*>(at);
-        return p[0] | (second ? (uint32_t)p[1] << 16 : 0u);
-    }
     static __device__ __forceinline__ P2 get(Raw r) { return pair(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u)); }
-    static __device__ __forceinline__ void store(char* at, bool second, P2 v) {
+    template <bool VEC> static __device__ __forceinline__ void store(char* at, bool second, P2 v) {
         const float2 f = both(v);
         __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(at);
         if (VEC) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(f.x, f.y); return; }
@@ -95,16 +89,10 @@ template <bool VEC> struct Two<__nv_bfloat16, VEC> {
         if (second) p[1] = __float2bfloat16_rn(f.y);
     }
 };
-template <bool VEC> struct Two<float, VEC> {
+template <> struct Two<float> {
     using Raw = P2;
-    static __device__ __forceinline__ Raw none() { return 0; }
-    static __device__ __forceinline__ Raw load(const char* at, bool second) {
-        if (VEC) return __ldg(reinterpret_cast<const unsigned long long*>(at));
-        const float* p = reinterpret_cast<const float*>(at);
-        return pair(p[0], second ? p[1] : 0.f);
-    }
     static __device__ __forceinline__ P2 get(Raw r) { return r; }
-    static __device__ __forceinline__ void store(char* at, bool second, P2 v) {
+    template <bool VEC> static __device__ __forceinline__ void store(char* at, bool second, P2 v) {
         if (VEC) { *reinterpret_cast<P2*>(at) = v; return; }
         const float2 f = both(v);
         float* p = reinterpret_cast<float*>(at);
@@ -112,6 +100,64 @@ template <bool VEC> struct Two<float, VEC> {
         if (second) p[1] = f.y;
     }
 };
+
+// Tokens on their way into shared memory.  Each warp has kStages buffers of its own for the tokens of its two runs (so that nothing but the
+// warp waits for them), each of a row of kTile channels per token and input; a lane copies two pieces of 16 bytes of every input.
+template <typename T>
+struct Stage {
+    static constexpr int kRowBytes = kTile * (int)sizeof(T), kRun = kRunOf<T>;
+    static constexpr int kRunBytes = kRun * kRowBytes + (kRowBytes < 128 ? kRowBytes : 0);      // the two runs on different banks
+    static constexpr int kBytes = 2 * kRunBytes;                                                // one input, one stage
+    static constexpr int kPerRow = kRowBytes / 16, kHalf = 32 / kPerRow;                        // pieces of a row; rows that the warp copies at once
+};
+static_assert(Stage<float>::kHalf * 2 == 2 * kRunOf<float> && Stage<__nv_bfloat16>::kHalf * 2 == 2 * kRunOf<__nv_bfloat16>, "two pieces a lane");
+
+// One piece: 16 bytes from global to shared memory, the first `elements` of them (the rest zeros).
+template <typename T, bool VEC>
+__device__ __forceinline__ void copy16(uint32_t to, const char* from, int elements) {
+    if (VEC) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(elements > 0 ? 16 : 0) : "memory");
+    } else {
+        constexpr int n = 16 / (int)sizeof(T);
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+            if (i < elements) {
+                if (sizeof(T) == 2) w[i / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(from)[i] << (16 * (i & 1));
+                else w[i] = reinterpret_cast<const uint32_t*>(from)[i];
+            }
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+}
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void arrived() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
+    __syncwarp();
+}
+template <typename R> __device__ __forceinline__ R read(uint32_t at);
+template <> __device__ __forceinline__ uint32_t read<uint32_t>(uint32_t at) { uint32_t r; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r) : "r"(at)); return r; }
+template <> __device__ __forceinline__ P2 read<P2>(uint32_t at) { P2 r; asm volatile("ld.shared.u64 %0, [%1];" : "=l"(r) : "r"(at)); return r; }
+
+// One input of a block: where this lane's pieces are, token by token forwards (step > 0) or backwards.
+template <typename T, bool VEC>
+struct Input {
+    using S = Stage<T>;
+    const char* at;
+    long long step;           // bytes from a token to the next one in this order
+    __device__ __forceinline__ Input(const char* base, long long token0, long long step_, int lane32) : at(base + token0 * step_ + (lane32 / S::kPerRow) * step_ + (lane32 % S::kPerRow) * 16), step(step_) {}
+    // Copies the tokens first + (0 .. 2 kRun - 1) of the warp; tokens at `end` or behind are zeros, channels behind the last too.
+    __device__ __forceinline__ void fetch(uint32_t to, int first, int end, int channels, int lane32, int stride) {
+        const int row = lane32 / S::kPerRow, col = lane32 % S::kPerRow, left = channels - col * (16 / (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = row + i * S::kHalf;
+            const bool in = first + r < end;
+            copy16<T, VEC>(to + (r / S::kRun) * S::kRunBytes + (r % S::kRun) * S::kRowBytes + col * 16, in && left > 0 ? at + i * S::kHalf * step : at, in ? left : 0);
+        }
+        at += stride * step;
+    }
+};
+
 // fp32 values of a state [B][C].
 __device__ __forceinline__ P2 load_state(const float* p, size_t i, bool live, bool second) {
     return p && live ? pair(p[i], second ? p[i + 1] : 0.f) : 0;
@@ -223,50 +269,48 @@ struct Cluster {
 
 template <typename T, int GATE, bool CONVEX, bool VEC>
 __global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_constant__ Args p) {
-    using V = Two<T, VEC>;
-    constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>;
+    using V = Two<T>;
+    using S = Stage<T>;
+    constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>, kInputs = 2, kStages = 3;
     __shared__ Exchange e;
+    extern __shared__ __align__(128) char staged[];
     Cluster cl(e);
-    const int c = blockIdx.y * kTile + 2 * cl.lane, b = blockIdx.z;
+    const int lane32 = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.y * kTile + 2 * cl.lane, b = blockIdx.z;
+    const int channels = p.C - (int)blockIdx.y * kTile;
     const bool live = c < p.C, second = c + 1 < p.C;
     const size_t at_state = (size_t)b * p.C + c;
     P2 carry = load_state(p.in, at_state, live, second);
     const long long gs = p.g_token * (int)sizeof(T), xs = p.x_token * (int)sizeof(T), os = (long long)p.C * (int)sizeof(T);
-    int t0 = cl.rank * kPiece + cl.run * kRun;
-    const int stride = cl.blocks * kPiece;
-    const char* pg = p.g + (b * p.g_batch + c) * (int)sizeof(T) + t0 * gs;
-    const char* px = p.x + (b * p.x_batch + c) * (int)sizeof(T) + t0 * xs;
+    const int stride = cl.blocks * kPiece, tile = (int)blockIdx.y * kTile;
+    int w0 = cl.rank * kPiece + warp * 2 * kRun, t0 = w0 + (cl.run & 1) * kRun;      // first token of the warp, of the thread
+    Input<T, VEC> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T), w0, gs, lane32), x(p.x + (b * p.x_batch + tile) * (int)sizeof(T), w0, xs, lane32);
     char* po = p.out0 + ((long long)b * p.N * p.C + c) * (int)sizeof(T) + t0 * os;
-    typename V::Raw rg[kRun], rx[kRun];
-    auto fetch = [&](int t) {
-        if (live && t + kRun <= p.N) {
-#pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                rg[k] = V::load(pg + k * gs, second);
-                rx[k] = V::load(px + k * xs, second);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                const bool in = live && t + k < p.N;
-                rg[k] = in ? V::load(pg + k * gs, second) : V::none();
-                rx[k] = in ? V::load(px + k * xs, second) : V::none();
-            }
+    const uint32_t mine = tc::smem_u32(staged) + warp * (kStages * kInputs * S::kBytes), own = (cl.run & 1) * S::kRunBytes + cl.lane * 2 * (int)sizeof(T);
+    auto fetch = [&](int piece, int stage) {
+        if (piece < p.pieces) {
+            const uint32_t to = mine + stage * (kInputs * S::kBytes);
+            g.fetch(to, w0 + piece * stride, p.N, channels, lane32, stride);
+            x.fetch(to + S::kBytes, w0 + piece * stride, p.N, channels, lane32, stride);
         }
-        pg += stride * gs;
-        px += stride * xs;
+        commit();
     };
-    fetch(t0);
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) fetch(i, i);
     cl.start();
-    for (int s = 0; s < p.pieces; ++s) {
+    for (int s = 0, stage = 0; s < p.pieces; ++s) {
+        arrived<kStages - 1>();
+        const uint32_t from = mine + stage * (kInputs * S::kBytes) + own;
         P2 a[kRun], u[kRun];
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
             P2 rest;
-            gate<GATE>(V::get(rg[k]), a[k], rest);
-            u[k] = V::get(rx[k]);
+            gate<GATE>(V::get(read<typename V::Raw>(from + k * S::kRowBytes)), a[k], rest);
+            u[k] = V::get(read<typename V::Raw>(from + S::kBytes + k * S::kRowBytes));
             if (CONVEX) u[k] = mul2(rest, u[k]);
         }
+        __syncwarp();
+        fetch(s + kStages, stage);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
         const bool whole = live && t0 + kRun <= p.N;
         if (!whole) {      // behind the end nothing changes
 #pragma unroll
@@ -279,19 +323,18 @@ __global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_const
             H = fma2(a[k], H, u[k]);
             A = mul2(a[k], A);
         }
-        if (s + 1 < p.pieces) fetch(t0 + stride);
         P2 h = cl.state_before(A, H, carry, s);
         if (whole) {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
                 h = fma2(a[k], h, u[k]);
-                V::store(po + k * os, second, h);
+                V::template store<VEC>(po + k * os, second, h);
             }
         } else if (live) {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
                 h = fma2(a[k], h, u[k]);
-                if (t0 + k < p.N) V::store(po + k * os, second, h);
+                if (t0 + k < p.N) V::template store<VEC>(po + k * os, second, h);
             }
         }
         po += stride * os;
@@ -303,84 +346,75 @@ __global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_const
 
 // Tokens are counted from the end: i = N - 1 - t; pointers go down.
 template <typename T, int GATE, bool CONVEX, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_constant__ Args p) {
-    using V = Two<T, VEC>;
+__global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_constant__ Args p) {
+    using V = Two<T>;
     using Raw = typename V::Raw;
-    constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>;
+    using S = Stage<T>;
+    constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>, kInputs = CONVEX ? 4 : 3, kStages = 2;
     __shared__ Exchange e;
+    extern __shared__ __align__(128) char staged[];
     Cluster cl(e);
-    const int c = blockIdx.y * kTile + 2 * cl.lane, b = blockIdx.z;
+    const int lane32 = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.y * kTile + 2 * cl.lane, b = blockIdx.z;
+    const int channels = p.C - (int)blockIdx.y * kTile;
     const bool live = c < p.C, second = c + 1 < p.C;
     const size_t at_state = (size_t)b * p.C + c;
     P2 carry = load_state(p.in, at_state, live, second);
     const P2 h0 = load_state(p.h0, at_state, live, second);
     const long long gs = p.g_token * (int)sizeof(T), xs = p.x_token * (int)sizeof(T), os = (long long)p.C * (int)sizeof(T);
-    int i0 = cl.rank * kPiece + cl.run * kRun;
-    const int stride = cl.blocks * kPiece;
-    const long long t_first = p.N - 1 - i0;
-    const char* pg = p.g + (b * p.g_batch + c) * (int)sizeof(T) + t_first * gs;
-    const char* px = CONVEX ? p.x + (b * p.x_batch + c) * (int)sizeof(T) + t_first * xs : nullptr;
-    const long long dense = ((long long)b * p.N * p.C + c) * (int)sizeof(T) + t_first * os;
-    const char *pd = p.dh + dense, *ph = p.h + dense - os;
-    char *po0 = p.out0 + dense, *po1 = p.out1 + dense;
-    Raw rg[kRun], rd[kRun];
-    auto fetch = [&](int i) {
-        if (live && i + kRun <= p.N) {
-#pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                rg[k] = V::load(pg - k * gs, second);
-                rd[k] = V::load(pd - k * os, second);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                const bool in = live && i + k < p.N;
-                rg[k] = in ? V::load(pg - k * gs, second) : V::none();
-                rd[k] = in ? V::load(pd - k * os, second) : V::none();
-            }
+    const int stride = cl.blocks * kPiece, tile = (int)blockIdx.y * kTile;
+    int w0 = cl.rank * kPiece + warp * 2 * kRun, i0 = w0 + (cl.run & 1) * kRun;
+    const long long dense = ((long long)b * p.N * p.C + tile) * (int)sizeof(T), end = p.N - 1;
+    Input<T, VEC> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T) + end * gs, w0, -gs, lane32), d(p.dh + dense + end * os, w0, -os, lane32),
+        h(p.h + dense + (end - 1) * os, w0, -os, lane32), x(CONVEX ? p.x + (b * p.x_batch + tile) * (int)sizeof(T) + end * xs : nullptr, w0, -xs, lane32);
+    const long long out = dense + 2 * cl.lane * (int)sizeof(T) + (end - i0) * os;
+    char *po0 = p.out0 + out, *po1 = p.out1 + out;
+    const uint32_t mine = tc::smem_u32(staged) + warp * (kStages * kInputs * S::kBytes), own = (cl.run & 1) * S::kRunBytes + cl.lane * 2 * (int)sizeof(T);
+    auto fetch = [&](int piece, int stage) {
+        if (piece < p.pieces) {
+            const uint32_t to = mine + stage * (kInputs * S::kBytes);
+            const int first = w0 + piece * stride;
+            g.fetch(to, first, p.N, channels, lane32, stride);
+            d.fetch(to + S::kBytes, first, p.N, channels, lane32, stride);
+            h.fetch(to + 2 * S::kBytes, first, p.N - 1, channels, lane32, stride);      // (the state before token 0 is h0)
+            if (CONVEX) x.fetch(to + 3 * S::kBytes, first, p.N, channels, lane32, stride);
         }
-        pg -= stride * gs;
-        pd -= stride * os;
+        commit();
     };
-    fetch(i0);
-    cl.start();
-    for (int s = 0; s < p.pieces; ++s) {
-        // what only the second going-through needs is on its way during the exchange
-        Raw rh[kRun], rx[kRun], now[kRun];
-        const bool whole = live && i0 + kRun < p.N;      // (the state before token 0 is h0)
 #pragma unroll
-        for (int k = 0; k < kRun; ++k) {
-            rh[k] = whole || (live && i0 + k + 1 < p.N) ? V::load(ph - k * os, second) : V::none();
-            rx[k] = CONVEX && (whole || (live && i0 + k < p.N)) ? V::load(px - k * xs, second) : V::none();
-        }
+    for (int i = 0; i < kStages; ++i) fetch(i, i);
+    cl.start();
+    for (int s = 0, stage = 0; s < p.pieces; ++s) {
+        arrived<kStages - 1>();
+        const uint32_t from = mine + stage * (kInputs * S::kBytes) + own;
+        const bool whole = live && i0 + kRun < p.N;
         P2 a[kRun], rest[kRun], A, M;
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
-            now[k] = rd[k];
-            gate<GATE>(V::get(rg[k]), a[k], rest[k]);
+            gate<GATE>(V::get(read<Raw>(from + k * S::kRowBytes)), a[k], rest[k]);
             if (!whole && i0 + k >= p.N) a[k] = twice(1.f);      // (its dh was not read and is zero)
-            const P2 d = V::get(now[k]);
-            M = mul2(a[k], k ? add2(d, M) : d);
+            const P2 dk = V::get(read<Raw>(from + S::kBytes + k * S::kRowBytes));
+            M = mul2(a[k], k ? add2(dk, M) : dk);
             A = k ? mul2(a[k], A) : a[k];
         }
-        if (s + 1 < p.pieces) fetch(i0 + stride);
         P2 mu = cl.state_before(A, M, carry, s);
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
-            const P2 lam = add2(V::get(now[k]), mu);
+            const P2 lam = add2(V::get(read<Raw>(from + S::kBytes + k * S::kRowBytes)), mu);
             mu = mul2(a[k], lam);
-            P2 w = !whole && i0 + k == p.N - 1 ? h0 : V::get(rh[k]);
-            if (CONVEX) w = fma2(V::get(rx[k]), twice(-1.f), w);
+            P2 w = V::get(read<Raw>(from + 2 * S::kBytes + k * S::kRowBytes));
+            if (!whole && i0 + k == p.N - 1) w = h0;
+            if (CONVEX) w = fma2(V::get(read<Raw>(from + 3 * S::kBytes + k * S::kRowBytes)), twice(-1.f), w);
             P2 dg = mul2(mu, w);      // lambda a (h_{t-1} - x)
             if (GATE == kSigmoid) dg = mul2(dg, rest[k]);
             const P2 dx = CONVEX ? mul2(lam, rest[k]) : lam;
             if (whole || (live && i0 + k < p.N)) {
-                V::store(po0 - k * os, second, dx);
-                V::store(po1 - k * os, second, dg);
+                V::template store<VEC>(po0 - k * os, second, dx);
+                V::template store<VEC>(po1 - k * os, second, dg);
             }
         }
-        ph -= stride * os;
-        px -= CONVEX ? stride * xs : 0;
+        __syncwarp();
+        fetch(s + kStages, stage);
+        stage ^= 1;
         po0 -= stride * os;
         po1 -= stride * os;
         i0 += stride;
@@ -388,6 +422,9 @@ __global__ void __launch_bounds__(kThreads, 2) backward_kernel(const __grid_cons
     if (p.last && cl.rank == 0 && cl.run == 0 && live) store_state(p.last, at_state, second, carry);
     cluster_sync();
 }
+
+template <typename T> constexpr int forward_bytes() { return kThreads / 32 * 3 * 2 * Stage<T>::kBytes; }
+template <typename T> constexpr int backward_bytes(bool convex) { return kThreads / 32 * 2 * (convex ? 4 : 3) * Stage<T>::kBytes; }
 
 }  // namespace scan
 }  // namespace hla
@@ -431,13 +468,14 @@ scan::Args common_args(const hla_scan* c) {
     return a;
 }
 
-// Whether two channels lie in one aligned word everywhere.
+// Whether rows consist of aligned 16-byte pieces everywhere: then they are copied asynchronously; else element by element.  (The dense tensors'
+// rows, C elements, are told by C.)
 bool vectors(const hla_scan* c, const scan::Args& a) {
-    const uintptr_t word = 2 * elt_size(c->cfg.dtype), at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.g);
-    return !((a.C | a.x_batch | a.x_token | a.g_batch | a.g_token) & 1) && at % word == 0;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.g);
+    return !((a.C | a.x_batch | a.x_token | a.g_batch | a.g_token) * elt_size(c->cfg.dtype) & 15) && at % 16 == 0;
 }
 
-hla_status launch(const hla_scan* c, Kernel kern, scan::Args& a, cudaStream_t st) {
+hla_status launch(const hla_scan* c, Kernel kern, int bytes, scan::Args& a, cudaStream_t st) {
     int blocks = 1;      // of a cluster
     const int piece = c->cfg.dtype == HLA_BF16 ? scan::kPieceOf<__nv_bfloat16> : scan::kPieceOf<float>;
     while (blocks < scan::kMaxCluster && blocks * piece < a.N) blocks *= 2;
@@ -445,7 +483,9 @@ hla_status launch(const hla_scan* c, Kernel kern, scan::Args& a, cudaStream_t st
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks, (a.C + scan::kTile - 1) / scan::kTile, c->cfg.B);
     cfg.blockDim = dim3(scan::kThreads);
+    cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return HLA_ERR_CUDA;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = blocks;
@@ -499,7 +539,7 @@ hla_status hla_scan_forward(hla_scan* c, const void* x, const void* g, const voi
     a.out0 = static_cast<char*>(h);
     a.in = static_cast<const float*>(h0);
     a.last = static_cast<float*>(h_last);
-    return launch(c, pick<Fwd>(c->cfg, vectors(c, a)), a, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, pick<Fwd>(c->cfg, vectors(c, a)), c->cfg.dtype == HLA_BF16 ? scan::forward_bytes<__nv_bfloat16>() : scan::forward_bytes<float>(), a, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const void* h0, const void* h, const void* dh, const void* dh_last,
@@ -535,7 +575,7 @@ hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const vo
     a.in = static_cast<const float*>(dh_last);
     a.h0 = static_cast<const float*>(h0);
     a.last = static_cast<float*>(dh0);
-    return launch(c, pick<Bwd>(c->cfg, vectors(c, a)), a, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, pick<Bwd>(c->cfg, vectors(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_destroy(hla_scan* c) {
