@@ -44,7 +44,7 @@ struct Tensor {
     float *ms, *vs;
     long long n;
     float lr_mul, decay;
-    uint32_t first;      // its first chunk in the launch
+    uint32_t first;      // its first unit in the launch
     uint32_t number;     // its place in the caller's list
     uint16_t p_bf16, g_bf16;
 };
@@ -52,7 +52,8 @@ struct Tensor {
 template <int MANY>
 struct Args {
     int n;                        // tensors of this launch
-    uint32_t chunks;
+    uint32_t units;               // turns: up to `span` chunks of a tensor each
+    int span;
     int norm_blocks;              // partial sums of the squared norm (0: no norm)
     double* part;
     float* norm_out;
@@ -75,7 +76,7 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-// The tensor that chunk c belongs to, from the one that an earlier chunk belonged to on.
+// The tensor that unit c belongs to, from the one that an earlier unit belonged to on.
 template <int MANY>
 __device__ __forceinline__ int tensor_of(const Args<MANY>& a, uint32_t c, int from) {
     if (from + 1 >= a.n || c < a.t[from + 1].first) return from;
@@ -87,69 +88,72 @@ __device__ __forceinline__ int tensor_of(const Args<MANY>& a, uint32_t c, int fr
     return lo;
 }
 
-// Four elements at `i` of a tensor with `n` elements in all, as raw words; elements behind the end are zeros.
-template <bool NC>
+// Four elements at `i` of a tensor with `n` elements in all, as raw words; elements behind the end are zeros.  WHOLE: none are.
+template <bool WHOLE>
 __device__ __forceinline__ uint4 load_f32(const void* base, long long i, long long n) {
     const float* p = static_cast<const float*>(base) + i;
-    if (i + 4 <= n) return NC ? ld_once(reinterpret_cast<const uint4*>(p)) : *reinterpret_cast<const uint4*>(p);
+    if (WHOLE || i + 4 <= n) return *reinterpret_cast<const uint4*>(p);
     uint4 r = make_uint4(0, 0, 0, 0);
     if (i < n) r.x = __float_as_uint(p[0]);
     if (i + 1 < n) r.y = __float_as_uint(p[1]);
     if (i + 2 < n) r.z = __float_as_uint(p[2]);
     return r;
 }
-template <bool NC>
+template <bool WHOLE>
 __device__ __forceinline__ uint2 load_bf16(const void* base, long long i, long long n) {
     const unsigned short* p = static_cast<const unsigned short*>(base) + i;
-    if (i + 4 <= n) return NC ? ld_once(reinterpret_cast<const uint2*>(p)) : *reinterpret_cast<const uint2*>(p);
+    if (WHOLE || i + 4 <= n) return *reinterpret_cast<const uint2*>(p);
     uint2 r = make_uint2(0, 0);
     if (i < n) r.x = p[0];
     if (i + 1 < n) r.x |= (uint32_t)p[1] << 16;
     if (i + 2 < n) r.y = p[2];
     return r;
 }
+template <bool WHOLE>
 __device__ __forceinline__ uint32_t load_b8(const void* base, long long i, long long n) {
     const unsigned char* p = static_cast<const unsigned char*>(base) + i;
-    if (i + 4 <= n) return *reinterpret_cast<const uint32_t*>(p);
+    if (WHOLE || i + 4 <= n) return *reinterpret_cast<const uint32_t*>(p);
     uint32_t r = 0;
     if (i < n) r = p[0];
     if (i + 1 < n) r |= (uint32_t)p[1] << 8;
     if (i + 2 < n) r |= (uint32_t)p[2] << 16;
     return r;
 }
-// Four floats or bf16 values; the type is a property of the tensor (the same for a whole block).
-template <bool NC>
-__device__ __forceinline__ uint4 load_any(const void* base, bool bf16, long long i, long long n) {
-    if (bf16) {
-        const uint2 r = load_bf16<NC>(base, i, n);
-        return make_uint4(r.x, r.y, 0, 0);
-    }
-    return load_f32<NC>(base, i, n);
+// Four floats or bf16 values.
+template <bool BF16, bool WHOLE>
+__device__ __forceinline__ uint4 load_any(const void* base, long long i, long long n) {
+    if (!BF16) return load_f32<WHOLE>(base, i, n);
+    const uint2 r = load_bf16<WHOLE>(base, i, n);
+    return make_uint4(r.x, r.y, 0, 0);
 }
-__device__ __forceinline__ void unpack(const uint4& r, bool bf16, float (&x)[4]) {
-    if (bf16) {
+template <bool BF16>
+__device__ __forceinline__ void unpack(const uint4& r, float (&x)[4]) {
+    if (BF16) {
         x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xffff0000u);
         x[2] = __uint_as_float(r.y << 16); x[3] = __uint_as_float(r.y & 0xffff0000u);
     } else {
         x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
     }
 }
+template <bool WHOLE>
 __device__ __forceinline__ void store_f32(void* base, long long i, long long n, const float (&x)[4]) {
     float* p = static_cast<float*>(base) + i;
-    if (i + 4 <= n) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); return; }
+    if (WHOLE || i + 4 <= n) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); return; }
     for (int j = 0; j < 3; ++j)
         if (i + j < n) p[j] = x[j];
 }
+template <bool WHOLE>
 __device__ __forceinline__ void store_bf16(void* base, long long i, long long n, uint32_t lo, uint32_t hi) {
     unsigned short* p = static_cast<unsigned short*>(base) + i;
-    if (i + 4 <= n) { *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi); return; }
+    if (WHOLE || i + 4 <= n) { *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi); return; }
     if (i < n) p[0] = (unsigned short)lo;
     if (i + 1 < n) p[1] = (unsigned short)(lo >> 16);
     if (i + 2 < n) p[2] = (unsigned short)hi;
 }
+template <bool WHOLE>
 __device__ __forceinline__ void store_b8(void* base, long long i, long long n, uint32_t c) {
     unsigned char* p = static_cast<unsigned char*>(base) + i;
-    if (i + 4 <= n) { *reinterpret_cast<uint32_t*>(p) = c; return; }
+    if (WHOLE || i + 4 <= n) { *reinterpret_cast<uint32_t*>(p) = c; return; }
     if (i < n) p[0] = (unsigned char)c;
     if (i + 1 < n) p[1] = (unsigned char)(c >> 8);
     if (i + 2 < n) p[2] = (unsigned char)(c >> 16);
@@ -180,20 +184,38 @@ __device__ __forceinline__ float row_max(const float (&x)[4]) {
     return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));      // (bits of non-negative floats are ordered like them)
 }
 
-// A value as e4m3, rounded by the 20 random bits `r`, in the top byte of the result.  x * inv is at most 448; times 2^-120 the smallest
+// 448 / most, never above it (x / most * 448 must not pass 448): the reciprocal's error of 2^-23 is taken off.
+__device__ __forceinline__ float codes_per_unit(float most) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(most * 0.25f));      // (a quarter: the reciprocal of the largest floats would be flushed)
+    return r * (112.f * (1.f - 0x1p-21f));
+}
+
+// A value as e4m3, rounded by the 20 random bits `r`, in the top byte of the result (sign included).  With x / scale times 2^-120 the smallest
 // normal e4m3 falls on the smallest normal fp32, so that one addition to the bits rounds normal and subnormal codes alike.
-__device__ __forceinline__ uint32_t round_q8(float x, float inv, uint32_t r) {
-    const uint32_t w = __float_as_uint(__fmul_rn(__fmul_rn(x, inv), 7.52316384526264e-37f)) + r;
+__device__ __forceinline__ uint32_t round_q8(float scaled, uint32_t r) {
+    const uint32_t w = __float_as_uint(scaled) + r;
     return (w & 0x80000000u) | (w << 4);
 }
 __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&w)[4]) {
     return __byte_perm(__byte_perm(w[0], w[1], 0x0073), __byte_perm(w[2], w[3], 0x0073), 0x5410);
 }
+// x / scale times 2^-120 for a row whose largest entry is `most`: in one product where the factor is a normal number.
+__device__ __forceinline__ void scaled_row(const float (&x)[4], float most, float (&y)[4]) {
+    const float per = codes_per_unit(most);
+    if (most < 16384.f) {
+        const float f = per * 0x1p-120f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = x[j] * f;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = x[j] * per * 0x1p-120f;
+    }
+}
 
 // The scale of a row whose largest entry is `most`.  A row with an entry that is no number, or infinite, is no numbers throughout.
 __device__ __forceinline__ float scale_of(float most) {
-    if (most < kDead) return 0.f;
-    return most <= 3.402823466e38f ? most / 448.f : __int_as_float(0x7fc00000);
+    return most < kDead ? 0.f : most <= 3.402823466e38f ? most * (1.f / 448.f) : __int_as_float(0x7fc00000);
 }
 
 __device__ __forceinline__ float sqrt_fast(float x) {
@@ -215,27 +237,63 @@ __device__ __forceinline__ double block_total(const double* part, int count, dou
     return v;
 }
 
-// Squares are summed in 64 bits: large gradients cannot overflow the sum, and a step does not depend on how it was cut.
+// What a block does of a tensor in one turn: `whole` chunks, then the tensor's last, incomplete one if `rest`.
+struct Share {
+    long long first;      // of this lane
+    int whole, rest;
+    __device__ __forceinline__ Share(const Tensor& t, uint32_t unit, int span, int warp, int lane) {
+        const long long begin = (long long)(unit - t.first) * span * kChunk, left = t.n - begin;
+        first = begin + warp * (kRows * kRow) + lane * 4;
+        whole = left >= (long long)span * kChunk ? span : (int)(left / kChunk);
+        rest = whole < span && left > (long long)whole * kChunk;
+    }
+};
+
+// The squares of four elements, in 64 bits.  Formed in fp32 where they and their sum are normal there; huge and tiny gradients are squared
+// in 64 bits.
+__device__ __forceinline__ double squares(const float (&g)[4]) {
+    const float q = fmaf(g[0], g[0], g[1] * g[1]) + fmaf(g[2], g[2], g[3] * g[3]);
+    if (q > 1e-25f && q < 1e38f) return q;
+    double v = 0.0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v = fma((double)g[j], (double)g[j], v);
+    return v;
+}
+
+// A warp's share of `count` chunks of a tensor from element `first` on (of this lane).
+template <bool BF16, bool WHOLE>
+__device__ __forceinline__ double run_squares(const Tensor& t, long long first, int count) {
+    const char* at = static_cast<const char*>(t.g) + first * (BF16 ? 2 : 4);
+    double sum = 0.0;
+    for (; count > 0; --count) {
+        uint4 raw[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) raw[r] = load_any<BF16, WHOLE>(at, r * kRow, t.n - first);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            float g[4];
+            unpack<BF16>(raw[r], g);
+            sum += squares(g);
+        }
+        at += kChunk * (BF16 ? 2 : 4);
+        first += kChunk;
+    }
+    return sum;
+}
+
+// Sums of squares run in 64 bits: the norm does not overflow where its gradients do not, and hardly depends on how the tensors were cut.
 template <int MANY>
 __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ Args<MANY> a) {
     __shared__ double scratch[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     double sum = 0.0;
     int at = 0;
-    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+    for (uint32_t c = blockIdx.x; c < a.units; c += gridDim.x) {
         at = tensor_of(a, c, at);
         const Tensor& t = a.t[at];
-        const long long first = (long long)(c - t.first) * kChunk + warp * (kRows * kRow) + lane * 4;
-        uint4 raw[kRows];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) raw[r] = load_any<false>(t.g, t.g_bf16, first + r * kRow, t.n);
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            float g[4];
-            unpack(raw[r], t.g_bf16, g);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum = fma((double)g[j], (double)g[j], sum);
-        }
+        const Share s(t, c, a.span, warp, lane);
+        if (s.whole) sum += t.g_bf16 ? run_squares<true, true>(t, s.first, s.whole) : run_squares<false, true>(t, s.first, s.whole);
+        if (s.rest) sum += t.g_bf16 ? run_squares<true, false>(t, s.first + s.whole * (long long)kChunk, 1) : run_squares<false, false>(t, s.first + s.whole * (long long)kChunk, 1);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -246,6 +304,139 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
         for (int w = 0; w < kWarps; ++w) sum += scratch[w];
         a.part[blockIdx.x] = sum;
     }
+}
+
+struct Coefficients {
+    float gain, b1, r1, b2, r2, eps, lr, inv1, inv2;
+    uint32_t key;
+};
+
+// The rows of a warp in `count` chunks, from element `first` (of this lane) on.  WHOLE: all of them lie in the tensor.
+template <bool Q8, bool PB, bool GB, bool WHOLE>
+__device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, long long first, int count, int lane) {
+    constexpr int kP = PB ? 2 : 4, kG = GB ? 2 : 4, kS = Q8 ? 1 : 4;
+    const char* pg = static_cast<const char*>(t.g) + first * kG;
+    char *pp = static_cast<char*>(t.p) + first * kP, *pm = static_cast<char*>(t.m) + first * kS, *pv = static_cast<char*>(t.v) + first * kS;
+    char* pc = PB || !t.copy ? nullptr : static_cast<char*>(t.copy) + first * 2;
+    uint32_t row0 = (uint32_t)(first / kRow);      // (tensors have up to 2^38 elements)
+    float *pms = Q8 ? t.ms + row0 : nullptr, *pvs = Q8 ? t.vs + row0 : nullptr;
+    long long n = t.n - first;                     // elements from this lane's first on
+    const float rate = k.lr * t.lr_mul, size = rate * k.inv1, shrink = rate * t.decay;
+    const uint32_t tensor_key = Q8 || PB ? mix32(k.key + t.number) : 0;
+    for (; count > 0; --count) {
+        uint4 rg[kRows], rp[kRows], rm[kRows], rv[kRows];
+        uint32_t cm[kRows], cv[kRows];
+        float sm[kRows], sv[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int i = r * kRow;
+            rg[r] = load_any<GB, WHOLE>(pg, i, n);
+            rp[r] = load_any<PB, WHOLE>(pp, i, n);
+            if (Q8) {
+                const bool some = WHOLE || i - lane * 4 < n;
+                cm[r] = load_b8<WHOLE>(pm, i, n);
+                cv[r] = load_b8<WHOLE>(pv, i, n);
+                sm[r] = some ? pms[r] : 0.f;
+                sv[r] = some ? pvs[r] : 0.f;
+            } else {
+                rm[r] = load_f32<WHOLE>(pm, i, n);
+                rv[r] = load_f32<WHOLE>(pv, i, n);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int i = r * kRow;
+            float g[4], p[4], m[4], v[4];
+            unpack<GB>(rg[r], g);
+            unpack<PB>(rp[r], p);
+            float cb1 = k.b1, cb2 = k.b2;
+            if (Q8) {
+                decode2(cm[r], m[0], m[1]); decode2(cm[r] >> 16, m[2], m[3]);
+                decode2(cv[r], v[0], v[1]); decode2(cv[r] >> 16, v[2], v[3]);
+                cb1 *= sm[r];
+                cb2 *= sv[r];
+            } else {
+                unpack<false>(rm[r], m);
+                unpack<false>(rv[r], v);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g[j] *= k.gain;
+                m[j] = fmaf(k.r1, g[j], cb1 * m[j]);
+                v[j] = fmaf(k.r2 * g[j], g[j], cb2 * v[j]);
+                p[j] = fmaf(-size, __fdividef(m[j], fmaf(sqrt_fast(v[j]), k.inv2, k.eps)), fmaf(-shrink, p[j], p[j]));
+            }
+            uint32_t bits[4];
+            if (Q8 || PB) {
+                const uint32_t block = mix32(tensor_key + (row0 + r) * 0x9E3779B9u) + (uint32_t)lane * 2u * 0x9E3779B9u;
+#pragma unroll
+                for (int j = 0; j < 4; j += 2) {
+                    uint32_t x = block + (uint32_t)(j / 2) * 0x9E3779B9u;
+                    x ^= x >> 16;
+                    x *= 0x7FEB352Du;
+                    x = (x ^ (x >> 15)) * 0x846CA68Bu;
+                    const uint32_t y = x * 0xC2B2AE35u;
+                    bits[j] = x ^ (x >> 16);
+                    bits[j + 1] = y ^ (y >> 15);
+                }
+            }
+            if (PB) {
+                uint32_t h[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    h[j] = __float_as_uint(p[j]);
+                    if (p[j] == p[j]) h[j] += bits[j] * 0x9E3779B9u >> 16;      // (an infinity has no low bits to carry from; a NaN would overflow)
+                }
+                store_bf16<WHOLE>(pp, i, n, __byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x7632));
+            } else {
+                store_f32<WHOLE>(pp, i, n, p);
+                if (pc) store_bf16<WHOLE>(pc, i, n, two_bf16(p[0], p[1]), two_bf16(p[2], p[3]));
+            }
+            if (!Q8) {
+                store_f32<WHOLE>(pm, i, n, m);
+                store_f32<WHOLE>(pv, i, n, v);
+            } else {
+                const float mm = row_max(m), mv = row_max(v);
+                uint32_t qm = 0, qv = 0;
+                if (mm >= kDead && mm <= 3.402823466e38f) {
+                    float y[4];
+                    uint32_t w[4];
+                    scaled_row(m, mm, y);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = round_q8(y[j], bits[j] & 0xfffffu);
+                    qm = top_bytes(w);
+                }
+                if (mv >= kDead && mv <= 3.402823466e38f) {
+                    float y[4];
+                    uint32_t w[4];
+                    scaled_row(v, mv, y);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = max((__float_as_uint(y[j]) + (bits[j] >> 12)) << 4, v[j] > 0.f ? 1u << 24 : 0u);
+                    qv = top_bytes(w);
+                }
+                store_b8<WHOLE>(pm, i, n, qm);
+                store_b8<WHOLE>(pv, i, n, qv);
+                if (lane == 0 && (WHOLE || i < n)) {
+                    pms[r] = scale_of(mm);
+                    pvs[r] = scale_of(mv);
+                }
+            }
+        }
+        pg += kChunk * kG;
+        pp += kChunk * kP;
+        pm += kChunk * kS;
+        pv += kChunk * kS;
+        if (pc) pc += kChunk * 2;
+        if (Q8) { pms += kChunk / kRow; pvs += kChunk / kRow; }
+        row0 += kChunk / kRow;
+        n -= kChunk;
+    }
+}
+
+template <bool Q8, bool PB, bool GB>
+__device__ __forceinline__ void update_share(const Tensor& t, const Coefficients& k, const Share& s, int lane) {
+    if (s.whole) update<Q8, PB, GB, true>(t, k, s.first, s.whole, lane);
+    if (s.rest) update<Q8, PB, GB, false>(t, k, s.first + s.whole * (long long)kChunk, 1, lane);
 }
 
 template <int MANY, bool Q8>
@@ -259,120 +450,27 @@ __global__ void __launch_bounds__(kThreads, 4) step_kernel(const __grid_constant
         hyper[0] = (float)(-1.0 / expm1((double)step * log(a.beta1)));
         hyper[1] = (float)rsqrt(-expm1((double)step * log(a.beta2)));
     }
-    float gain = a.grad_scale;
+    Coefficients k;
+    k.gain = a.grad_scale;
     if (a.norm_blocks) {
         const float norm = (float)(sqrt(block_total(a.part, a.norm_blocks, scratch)) * fabs((double)a.grad_scale));
         if (blockIdx.x == 0 && threadIdx.x == 0 && a.norm_out) *a.norm_out = norm;
         if (!isfinite(norm)) return;      // nothing changes
-        gain *= fminf(a.max_norm / (norm + 1e-6f), 1.f);
+        k.gain *= fminf(a.max_norm / (norm + 1e-6f), 1.f);
     }
     __syncthreads();
-    const float lr = a.lr_device ? *a.lr_device : a.lr;
-    const float inv1 = a.step_device ? hyper[0] : a.inv1, inv2 = a.step_device ? hyper[1] : a.inv2;
-    const uint32_t key = mix32(mix32(mix32(a.seed_lo) ^ a.seed_hi) ^ (uint32_t)step);
+    k.b1 = a.b1; k.r1 = a.r1; k.b2 = a.b2; k.r2 = a.r2; k.eps = a.eps;
+    k.lr = a.lr_device ? *a.lr_device : a.lr;
+    k.inv1 = a.step_device ? hyper[0] : a.inv1;
+    k.inv2 = a.step_device ? hyper[1] : a.inv2;
+    k.key = mix32(mix32(mix32(a.seed_lo) ^ a.seed_hi) ^ (uint32_t)step);
     int at = 0;
-    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+    for (uint32_t c = blockIdx.x; c < a.units; c += gridDim.x) {
         at = tensor_of(a, c, at);
         const Tensor& t = a.t[at];
-        const long long n = t.n, row0 = (long long)(c - t.first) * (kWarps * kRows) + warp * kRows, first = row0 * kRow + lane * 4;
-        const bool pb = t.p_bf16, gb = t.g_bf16;
-        uint4 rg[kRows], rp[kRows], rm[kRows], rv[kRows];
-        uint32_t cm[kRows], cv[kRows];
-        float sm[kRows], sv[kRows];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const long long i = first + r * kRow;
-            rg[r] = load_any<false>(t.g, gb, i, n);
-            rp[r] = load_any<false>(t.p, pb, i, n);
-            if (Q8) {
-                const bool some = (row0 + r) * kRow < n;
-                cm[r] = load_b8(t.m, i, n);
-                cv[r] = load_b8(t.v, i, n);
-                sm[r] = some ? t.ms[row0 + r] : 0.f;
-                sv[r] = some ? t.vs[row0 + r] : 0.f;
-            } else {
-                rm[r] = load_f32<false>(t.m, i, n);
-                rv[r] = load_f32<false>(t.v, i, n);
-            }
-        }
-        const float rate = lr * t.lr_mul, size = rate * inv1, shrink = rate * t.decay;
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const long long i = first + r * kRow;
-            float g[4], p[4], m[4], v[4];
-            unpack(rg[r], gb, g);
-            unpack(rp[r], pb, p);
-            if (Q8) {
-                decode2(cm[r], m[0], m[1]); decode2(cm[r] >> 16, m[2], m[3]);
-                decode2(cv[r], v[0], v[1]); decode2(cv[r] >> 16, v[2], v[3]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { m[j] *= sm[r]; v[j] *= sv[r]; }
-            } else {
-                unpack(rm[r], false, m);
-                unpack(rv[r], false, v);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                g[j] *= gain;
-                m[j] = __fadd_rn(__fmul_rn(a.b1, m[j]), __fmul_rn(a.r1, g[j]));
-                v[j] = __fadd_rn(__fmul_rn(a.b2, v[j]), __fmul_rn(__fmul_rn(a.r2, g[j]), g[j]));
-                const float root = sqrt_fast(v[j]);
-                p[j] = fmaf(-shrink, p[j], p[j]) - size * __fdividef(m[j], fmaf(root, inv2, a.eps));
-            }
-            uint32_t bits[4];
-            if (Q8 || pb) {
-                const uint32_t block = mix32(mix32(key + t.number) + (uint32_t)(row0 + r) * 0x9E3779B9u);
-#pragma unroll
-                for (int j = 0; j < 4; j += 2) {
-                    uint32_t x = block + (uint32_t)(lane * 2 + j / 2) * 0x9E3779B9u;
-                    x ^= x >> 16;
-                    x *= 0x7FEB352Du;
-                    x = (x ^ (x >> 15)) * 0x846CA68Bu;
-                    const uint32_t y = x * 0xC2B2AE35u;
-                    bits[j] = x ^ (x >> 16);
-                    bits[j + 1] = y ^ (y >> 15);
-                }
-            }
-            if (pb) {
-                uint32_t h[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t w = __float_as_uint(p[j]);
-                    h[j] = (w & 0x7f800000u) == 0x7f800000u ? w : w + (bits[j] * 0x9E3779B9u >> 16);
-                }
-                store_bf16(t.p, i, n, __byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x7632));
-            } else {
-                store_f32(t.p, i, n, p);
-            }
-            if (t.copy) store_bf16(t.copy, i, n, two_bf16(p[0], p[1]), two_bf16(p[2], p[3]));
-            if (!Q8) {
-                store_f32(t.m, i, n, m);
-                store_f32(t.v, i, n, v);
-            } else {
-                const float mm = row_max(m), mv = row_max(v);
-                uint32_t qm = 0, qv = 0;
-                if (mm >= kDead && mm <= 3.402823466e38f) {
-                    const float inv = __fdiv_rz(448.f, mm);
-                    uint32_t w[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = round_q8(m[j], inv, bits[j] & 0xfffffu);
-                    qm = top_bytes(w);
-                }
-                if (mv >= kDead && mv <= 3.402823466e38f) {
-                    const float inv = __fdiv_rz(448.f, mv);
-                    uint32_t w[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = max(round_q8(v[j], inv, bits[j] >> 12), v[j] > 0.f ? 1u << 24 : 0u);
-                    qv = top_bytes(w);
-                }
-                store_b8(t.m, i, n, qm);
-                store_b8(t.v, i, n, qv);
-                if (lane == 0 && i < n) {
-                    t.ms[row0 + r] = scale_of(mm);
-                    t.vs[row0 + r] = scale_of(mv);
-                }
-            }
-        }
+        const Share s(t, c, a.span, warp, lane);
+        if (t.p_bf16) t.g_bf16 ? update_share<Q8, true, true>(t, k, s, lane) : update_share<Q8, true, false>(t, k, s, lane);
+        else t.g_bf16 ? update_share<Q8, false, true>(t, k, s, lane) : update_share<Q8, false, false>(t, k, s, lane);
     }
 }
 
@@ -426,14 +524,26 @@ hla_status check_spans(const hla_adamw* c) {
     return clash(spans) ? HLA_ERR_INVALID_ARG : HLA_OK;
 }
 
+// Chunks that a block takes in one turn.  Finding a tensor and its pointers costs about 80 instructions, ten an element of a chunk; where
+// every block has at least 16 turns, eight chunks share them.
+int span(const hla_adamw* c, int from, int n) {
+    long long chunks = 0;
+    for (int i = 0; i < n; ++i) chunks += (c->t[from + i].n + adamw::kChunk - 1) / adamw::kChunk;
+    int s = 1;
+    while (s < 8 && chunks >= 2ll * s * 16 * 4 * c->sm_count) s *= 2;
+    return s;
+}
+
 template <int MANY>
 void fill(adamw::Args<MANY>& a, const hla_adamw* c, int from, int n) {
     a.n = n;
-    a.chunks = 0;
+    a.span = span(c, from, n);
+    a.units = 0;
+    const long long per = (long long)a.span * adamw::kChunk;
     for (int i = 0; i < n; ++i) {
         a.t[i] = c->t[from + i];
-        a.t[i].first = a.chunks;
-        a.chunks += (uint32_t)((a.t[i].n + adamw::kChunk - 1) / adamw::kChunk);
+        a.t[i].first = a.units;
+        a.units += (uint32_t)((a.t[i].n + per - 1) / per);
     }
 }
 
@@ -443,7 +553,7 @@ int batch(const hla_adamw* c, int from) {
     return left < adamw::kMany ? left : adamw::kMany;
 }
 
-int norm_blocks(const hla_adamw* c, uint32_t chunks) { return (int)std::min<uint32_t>(chunks, 8u * c->sm_count); }
+int norm_blocks(const hla_adamw* c, uint32_t units) { return (int)std::min<uint32_t>(units, 8u * c->sm_count); }
 
 template <typename A>
 bool launch_step(void (*kern)(A), dim3 blocks, const A& a, cudaStream_t st) {
@@ -477,7 +587,7 @@ hla_status step(const hla_adamw* c, const hla_adamw_step_args& s, double* part, 
     if (s.max_norm > 0.f) {
         for (int from = 0; from < total; from += batch(c, from)) {
             fill(a, c, from, batch(c, from));
-            const int blocks = norm_blocks(c, a.chunks);
+            const int blocks = norm_blocks(c, a.units);
             a.part = part + a.norm_blocks;
             adamw::norm_kernel<MANY><<<blocks, adamw::kThreads, 0, st>>>(a);
             if (cudaGetLastError() != cudaSuccess) return HLA_ERR_CUDA;
@@ -488,7 +598,7 @@ hla_status step(const hla_adamw* c, const hla_adamw_step_args& s, double* part, 
     for (int from = 0; from < total; from += batch(c, from)) {
         fill(a, c, from, batch(c, from));
         if (from) a.norm_out = nullptr;
-        const dim3 blocks(std::min<uint32_t>(a.chunks, 4u * c->sm_count));
+        const dim3 blocks(std::min<uint32_t>(a.units, 4u * c->sm_count));
         const bool ok = k.state == HLA_STATE_Q8 ? launch_step(adamw::step_kernel<MANY, true>, blocks, a, st) : launch_step(adamw::step_kernel<MANY, false>, blocks, a, st);
         if (!ok) return HLA_ERR_CUDA;
     }
