@@ -46,7 +46,7 @@ struct Tensor {
     float lr_mul, decay;
     uint32_t first;      // its first unit in the launch
     uint32_t number;     // its place in the caller's list
-    uint16_t p_bf16, g_bf16;
+    uint8_t p_bf16, g_bf16;      // the same in all tensors of a launch
 };
 
 template <int MANY>
@@ -90,7 +90,7 @@ __device__ __forceinline__ int tensor_of(const Args<MANY>& a, uint32_t c, int fr
 
 // Four elements at `i` of a tensor with `n` elements in all, as raw words; elements behind the end are zeros.  WHOLE: none are.
 template <bool WHOLE>
-__device__ __forceinline__ uint4 load_f32(const void* base, long long i, long long n) {
+__device__ __forceinline__ uint4 load_f32(const void* base, int i, int n) {
     const float* p = static_cast<const float*>(base) + i;
     if (WHOLE || i + 4 <= n) return *reinterpret_cast<const uint4*>(p);
     uint4 r = make_uint4(0, 0, 0, 0);
@@ -100,7 +100,7 @@ __device__ __forceinline__ uint4 load_f32(const void* base, long long i, long lo
     return r;
 }
 template <bool WHOLE>
-__device__ __forceinline__ uint2 load_bf16(const void* base, long long i, long long n) {
+__device__ __forceinline__ uint2 load_bf16(const void* base, int i, int n) {
     const unsigned short* p = static_cast<const unsigned short*>(base) + i;
     if (WHOLE || i + 4 <= n) return *reinterpret_cast<const uint2*>(p);
     uint2 r = make_uint2(0, 0);
@@ -110,7 +110,7 @@ __device__ __forceinline__ uint2 load_bf16(const void* base, long long i, long l
     return r;
 }
 template <bool WHOLE>
-__device__ __forceinline__ uint32_t load_b8(const void* base, long long i, long long n) {
+__device__ __forceinline__ uint32_t load_b8(const void* base, int i, int n) {
     const unsigned char* p = static_cast<const unsigned char*>(base) + i;
     if (WHOLE || i + 4 <= n) return *reinterpret_cast<const uint32_t*>(p);
     uint32_t r = 0;
@@ -121,7 +121,7 @@ __device__ __forceinline__ uint32_t load_b8(const void* base, long long i, long 
 }
 // Four floats or bf16 values.
 template <bool BF16, bool WHOLE>
-__device__ __forceinline__ uint4 load_any(const void* base, long long i, long long n) {
+__device__ __forceinline__ uint4 load_any(const void* base, int i, int n) {
     if (!BF16) return load_f32<WHOLE>(base, i, n);
     const uint2 r = load_bf16<WHOLE>(base, i, n);
     return make_uint4(r.x, r.y, 0, 0);
@@ -136,14 +136,14 @@ __device__ __forceinline__ void unpack(const uint4& r, float (&x)[4]) {
     }
 }
 template <bool WHOLE>
-__device__ __forceinline__ void store_f32(void* base, long long i, long long n, const float (&x)[4]) {
+__device__ __forceinline__ void store_f32(void* base, int i, int n, const float (&x)[4]) {
     float* p = static_cast<float*>(base) + i;
     if (WHOLE || i + 4 <= n) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); return; }
     for (int j = 0; j < 3; ++j)
         if (i + j < n) p[j] = x[j];
 }
 template <bool WHOLE>
-__device__ __forceinline__ void store_bf16(void* base, long long i, long long n, uint32_t lo, uint32_t hi) {
+__device__ __forceinline__ void store_bf16(void* base, int i, int n, uint32_t lo, uint32_t hi) {
     unsigned short* p = static_cast<unsigned short*>(base) + i;
     if (WHOLE || i + 4 <= n) { *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi); return; }
     if (i < n) p[0] = (unsigned short)lo;
@@ -151,7 +151,7 @@ __device__ __forceinline__ void store_bf16(void* base, long long i, long long n,
     if (i + 2 < n) p[2] = (unsigned short)hi;
 }
 template <bool WHOLE>
-__device__ __forceinline__ void store_b8(void* base, long long i, long long n, uint32_t c) {
+__device__ __forceinline__ void store_b8(void* base, int i, int n, uint32_t c) {
     unsigned char* p = static_cast<unsigned char*>(base) + i;
     if (WHOLE || i + 4 <= n) { *reinterpret_cast<uint32_t*>(p) = c; return; }
     if (i < n) p[0] = (unsigned char)c;
@@ -172,56 +172,60 @@ __device__ __forceinline__ void decode2(uint32_t codes, float& x, float& y) {
     y = f.y;
 }
 
-__device__ __forceinline__ float max_abs(float a, float b) {      // a NaN stays
+__device__ __forceinline__ float max_abs(float a, float b, float c) {      // a NaN stays
     float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
-}
-
-// The largest of a row's |x| from every lane's own four; not a number if one of them is none.
-__device__ __forceinline__ float row_max(const float (&x)[4]) {
-    const float most = max_abs(max_abs(max_abs(fabsf(x[0]), x[1]), x[2]), x[3]);
-    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));      // (bits of non-negative floats are ordered like them)
-}
-
-// 448 / most, never above it (x / most * 448 must not pass 448): the reciprocal's error of 2^-23 is taken off.
-__device__ __forceinline__ float codes_per_unit(float most) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(most * 0.25f));      // (a quarter: the reciprocal of the largest floats would be flushed)
-    return r * (112.f * (1.f - 0x1p-21f));
-}
-
-// A value as e4m3, rounded by the 20 random bits `r`, in the top byte of the result (sign included).  With x / scale times 2^-120 the smallest
-// normal e4m3 falls on the smallest normal fp32, so that one addition to the bits rounds normal and subnormal codes alike.
-__device__ __forceinline__ uint32_t round_q8(float scaled, uint32_t r) {
-    const uint32_t w = __float_as_uint(scaled) + r;
-    return (w & 0x80000000u) | (w << 4);
-}
-__device__ __forceinline__ uint32_t top_bytes(const uint32_t (&w)[4]) {
-    return __byte_perm(__byte_perm(w[0], w[1], 0x0073), __byte_perm(w[2], w[3], 0x0073), 0x5410);
-}
-// x / scale times 2^-120 for a row whose largest entry is `most`: in one product where the factor is a normal number.
-__device__ __forceinline__ void scaled_row(const float (&x)[4], float most, float (&y)[4]) {
-    const float per = codes_per_unit(most);
-    if (most < 16384.f) {
-        const float f = per * 0x1p-120f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = x[j] * f;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = x[j] * per * 0x1p-120f;
-    }
-}
-
-// The scale of a row whose largest entry is `most`.  A row with an entry that is no number, or infinite, is no numbers throughout.
-__device__ __forceinline__ float scale_of(float most) {
-    return most < kDead ? 0.f : most <= 3.402823466e38f ? most * (1.f / 448.f) : __int_as_float(0x7fc00000);
 }
 
 __device__ __forceinline__ float sqrt_fast(float x) {
     float r;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// The largest of a row's |x| from every lane's own four; not a number if one of them is none.
+__device__ __forceinline__ float row_max(const float (&x)[4]) {
+    const float most = max_abs(max_abs(x[0], x[1], x[2]), x[3], x[3]);
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));      // (bits of non-negative floats are ordered like them)
+}
+
+// 448 / most times 2^-120, never above it (x / most * 448 must not pass 448): the reciprocal's error of 2^-23 is taken off.
+__device__ __forceinline__ float codes_per_unit(float most) { return reciprocal(most) * (448.f * (1.f - 0x1p-21f) * 0x1p-120f); }
+
+// Values as e4m3.  With x / scale times 2^-120 (`per` is that factor) the smallest normal e4m3 falls on the smallest normal fp32, so that one
+// addition of 20 random bits below the code's rounds normal and subnormal codes alike.  The code ends up in the top byte: integer
+// additions and shifts are what this kernel has too many of, so the shift is a product with the addition.
+__device__ __forceinline__ uint32_t top_bytes(const uint32_t (&w)[4]) {
+    return __byte_perm(__byte_perm(w[0], w[1], 0x0073), __byte_perm(w[2], w[3], 0x0073), 0x5410);
+}
+// The codes of four entries, of a moment that may be negative (low random bits) and of one that may not (high ones, and at least 1 where
+// the entry is not zero).
+__device__ __forceinline__ uint32_t codes(const float (&x)[4], float per, float less, const uint32_t (&bits)[4]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = (__float_as_uint(fabsf(x[j]) * less * per) * 16u + (bits[j] * 4096u >> 8)) | (__float_as_uint(x[j]) & 0x80000000u);
+    return top_bytes(w);
+}
+__device__ __forceinline__ uint32_t codes_positive(const float (&x)[4], float per, float less, const uint32_t (&bits)[4]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = max(__float_as_uint(x[j] * less * per), min(__float_as_uint(x[j]), 1u << 20)) * 16u + (bits[j] >> 8);
+    return top_bytes(w);
+}
+// Rows whose factor would not be a normal number (their largest entry from 2^14 on) are made smaller first.
+__device__ __forceinline__ bool usual(float most) { return most >= kDead && most < 16384.f; }
+__device__ __forceinline__ bool held(float most) { return most >= kDead && most <= 3.402823466e38f; }
+
+// The scale of a row whose largest entry is `most`.  A row with an entry that is no number, or infinite, is no numbers throughout.
+__device__ __forceinline__ float scale_of(float most) {
+    return most < kDead ? 0.f : most <= 3.402823466e38f ? most * (1.f / 448.f) : __int_as_float(0x7fc00000);
 }
 
 // The sum of the partial sums of the squared norm, in a fixed order, to every thread.
@@ -237,15 +241,17 @@ __device__ __forceinline__ double block_total(const double* part, int count, dou
     return v;
 }
 
-// What a block does of a tensor in one turn: `whole` chunks, then the tensor's last, incomplete one if `rest`.
+// What a block does of a tensor in one turn: `whole` chunks, then the tensor's last, incomplete one if there is a `rest`.
 struct Share {
-    long long first;      // of this lane
-    int whole, rest;
+    long long begin;      // its first element
+    int own;              // this lane's first element from there
+    int whole, rest;      // rest: elements of the incomplete chunk
     __device__ __forceinline__ Share(const Tensor& t, uint32_t unit, int span, int warp, int lane) {
-        const long long begin = (long long)(unit - t.first) * span * kChunk, left = t.n - begin;
-        first = begin + warp * (kRows * kRow) + lane * 4;
+        begin = (long long)(unit - t.first) * span * kChunk;
+        own = warp * (kRows * kRow) + lane * 4;
+        const long long left = t.n - begin;
         whole = left >= (long long)span * kChunk ? span : (int)(left / kChunk);
-        rest = whole < span && left > (long long)whole * kChunk;
+        rest = whole < span ? (int)(left - (long long)whole * kChunk) : 0;
     }
 };
 
@@ -260,29 +266,27 @@ __device__ __forceinline__ double squares(const float (&g)[4]) {
     return v;
 }
 
-// A warp's share of `count` chunks of a tensor from element `first` on (of this lane).
+// This lane's part of `count` chunks from `base` on, of `n` elements if not WHOLE.
 template <bool BF16, bool WHOLE>
-__device__ __forceinline__ double run_squares(const Tensor& t, long long first, int count) {
-    const char* at = static_cast<const char*>(t.g) + first * (BF16 ? 2 : 4);
+__device__ __forceinline__ double run_squares(const char* base, int own, int count, int n) {
     double sum = 0.0;
-    for (; count > 0; --count) {
+    base += own * (BF16 ? 2 : 4);
+    for (; count > 0; --count, base += kChunk * (BF16 ? 2 : 4)) {
         uint4 raw[kRows];
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) raw[r] = load_any<BF16, WHOLE>(at, r * kRow, t.n - first);
+        for (int r = 0; r < kRows; ++r) raw[r] = load_any<BF16, WHOLE>(base, r * kRow, n - own);
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             float g[4];
             unpack<BF16>(raw[r], g);
             sum += squares(g);
         }
-        at += kChunk * (BF16 ? 2 : 4);
-        first += kChunk;
     }
     return sum;
 }
 
 // Sums of squares run in 64 bits: the norm does not overflow where its gradients do not, and hardly depends on how the tensors were cut.
-template <int MANY>
+template <int MANY, bool GB>
 __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ Args<MANY> a) {
     __shared__ double scratch[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -292,8 +296,9 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
         at = tensor_of(a, c, at);
         const Tensor& t = a.t[at];
         const Share s(t, c, a.span, warp, lane);
-        if (s.whole) sum += t.g_bf16 ? run_squares<true, true>(t, s.first, s.whole) : run_squares<false, true>(t, s.first, s.whole);
-        if (s.rest) sum += t.g_bf16 ? run_squares<true, false>(t, s.first + s.whole * (long long)kChunk, 1) : run_squares<false, false>(t, s.first + s.whole * (long long)kChunk, 1);
+        const char* base = static_cast<const char*>(t.g) + s.begin * (GB ? 2 : 4);
+        if (s.whole) sum += run_squares<GB, true>(base, s.own, s.whole, 0);
+        if (s.rest) sum += run_squares<GB, false>(base + s.whole * (kChunk * (GB ? 2 : 4)), s.own, 1, s.rest);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -311,60 +316,77 @@ struct Coefficients {
     uint32_t key;
 };
 
-// The rows of a warp in `count` chunks, from element `first` (of this lane) on.  WHOLE: all of them lie in the tensor.
+// This lane's part of `count` chunks of a tensor from element `begin` on, of `n` elements if not WHOLE.
 template <bool Q8, bool PB, bool GB, bool WHOLE>
-__device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, long long first, int count, int lane) {
+__device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, long long begin, int own, int count, int n, int lane) {
     constexpr int kP = PB ? 2 : 4, kG = GB ? 2 : 4, kS = Q8 ? 1 : 4;
-    const char* pg = static_cast<const char*>(t.g) + first * kG;
-    char *pp = static_cast<char*>(t.p) + first * kP, *pm = static_cast<char*>(t.m) + first * kS, *pv = static_cast<char*>(t.v) + first * kS;
-    char* pc = PB || !t.copy ? nullptr : static_cast<char*>(t.copy) + first * 2;
-    uint32_t row0 = (uint32_t)(first / kRow);      // (tensors have up to 2^38 elements)
-    float *pms = Q8 ? t.ms + row0 : nullptr, *pvs = Q8 ? t.vs + row0 : nullptr;
-    long long n = t.n - first;                     // elements from this lane's first on
+    const char* pg = static_cast<const char*>(t.g) + begin * kG;
+    char *pp = static_cast<char*>(t.p) + begin * kP, *pm = static_cast<char*>(t.m) + begin * kS, *pv = static_cast<char*>(t.v) + begin * kS;
+    char* pc = PB || !t.copy ? nullptr : static_cast<char*>(t.copy) + begin * 2;
+    const uint32_t row_first = (uint32_t)(begin / kRow);      // (tensors have up to 2^38 elements)
+    float *pms = Q8 ? t.ms + row_first : nullptr, *pvs = Q8 ? t.vs + row_first : nullptr;
     const float rate = k.lr * t.lr_mul, size = rate * k.inv1, shrink = rate * t.decay;
     const uint32_t tensor_key = Q8 || PB ? mix32(k.key + t.number) : 0;
-    for (; count > 0; --count) {
-        uint4 rg[kRows], rp[kRows], rm[kRows], rv[kRows];
+    struct Raw {
+        uint4 g[kRows], p[kRows], m[kRows], v[kRows];
         uint32_t cm[kRows], cv[kRows];
         float sm[kRows], sv[kRows];
+    };
+    pg += own * kG;
+    pp += own * kP;
+    pm += own * kS;
+    pv += own * kS;
+    if (pc) pc += own * 2;
+    if (Q8) { pms += own / kRow; pvs += own / kRow; }
+    n -= own;
+    // the chunk that is `ahead` (0 or 1) chunks from here
+    auto load = [&](Raw& x, int ahead) {
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            const int i = r * kRow;
-            rg[r] = load_any<GB, WHOLE>(pg, i, n);
-            rp[r] = load_any<PB, WHOLE>(pp, i, n);
+            const int i = ahead * kChunk + r * kRow;
+            x.g[r] = load_any<GB, WHOLE>(pg, i, n);
+            x.p[r] = load_any<PB, WHOLE>(pp, i, n);
             if (Q8) {
                 const bool some = WHOLE || i - lane * 4 < n;
-                cm[r] = load_b8<WHOLE>(pm, i, n);
-                cv[r] = load_b8<WHOLE>(pv, i, n);
-                sm[r] = some ? pms[r] : 0.f;
-                sv[r] = some ? pvs[r] : 0.f;
+                x.cm[r] = load_b8<WHOLE>(pm, i, n);
+                x.cv[r] = load_b8<WHOLE>(pv, i, n);
+                x.sm[r] = some ? pms[i / kRow] : 0.f;
+                x.sv[r] = some ? pvs[i / kRow] : 0.f;
             } else {
-                rm[r] = load_f32<WHOLE>(pm, i, n);
-                rv[r] = load_f32<WHOLE>(pv, i, n);
+                x.m[r] = load_f32<WHOLE>(pm, i, n);
+                x.v[r] = load_f32<WHOLE>(pv, i, n);
             }
         }
+    };
+    // 8-bit states: the next chunk is on its way during the arithmetic of this one, which takes as long as its bytes
+    Raw raw, next;
+    if (Q8) load(raw, 0);
+    uint32_t row0 = row_first + own / kRow;
+    for (; count > 0; --count) {
+        if (!Q8) load(raw, 0);
+        else if (WHOLE && count > 1) load(next, 1);
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             const int i = r * kRow;
             float g[4], p[4], m[4], v[4];
-            unpack<GB>(rg[r], g);
-            unpack<PB>(rp[r], p);
+            unpack<GB>(raw.g[r], g);
+            unpack<PB>(raw.p[r], p);
             float cb1 = k.b1, cb2 = k.b2;
             if (Q8) {
-                decode2(cm[r], m[0], m[1]); decode2(cm[r] >> 16, m[2], m[3]);
-                decode2(cv[r], v[0], v[1]); decode2(cv[r] >> 16, v[2], v[3]);
-                cb1 *= sm[r];
-                cb2 *= sv[r];
+                decode2(raw.cm[r], m[0], m[1]); decode2(raw.cm[r] >> 16, m[2], m[3]);
+                decode2(raw.cv[r], v[0], v[1]); decode2(raw.cv[r] >> 16, v[2], v[3]);
+                cb1 *= raw.sm[r];
+                cb2 *= raw.sv[r];
             } else {
-                unpack<false>(rm[r], m);
-                unpack<false>(rv[r], v);
+                unpack<false>(raw.m[r], m);
+                unpack<false>(raw.v[r], v);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 g[j] *= k.gain;
                 m[j] = fmaf(k.r1, g[j], cb1 * m[j]);
                 v[j] = fmaf(k.r2 * g[j], g[j], cb2 * v[j]);
-                p[j] = fmaf(-size, __fdividef(m[j], fmaf(sqrt_fast(v[j]), k.inv2, k.eps)), fmaf(-shrink, p[j], p[j]));
+                p[j] = fmaf(-size, m[j] * reciprocal(fmaf(sqrt_fast(v[j]), k.inv2, k.eps)), fmaf(-shrink, p[j], p[j]));
             }
             uint32_t bits[4];
             if (Q8 || PB) {
@@ -382,10 +404,13 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
             }
             if (PB) {
                 uint32_t h[4];
+                const float any = (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    h[j] = __float_as_uint(p[j]);
-                    if (p[j] == p[j]) h[j] += bits[j] * 0x9E3779B9u >> 16;      // (an infinity has no low bits to carry from; a NaN would overflow)
+                for (int j = 0; j < 4; ++j) h[j] = __float_as_uint(p[j]) + (bits[j] * 0x9E3779B9u >> 16);
+                if (!(fabsf(any) <= 3.402823466e38f)) {      // an infinity has no low bits to carry from; a NaN would overflow
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (p[j] != p[j]) h[j] = __float_as_uint(p[j]);
                 }
                 store_bf16<WHOLE>(pp, i, n, __byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x7632));
             } else {
@@ -398,30 +423,26 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
             } else {
                 const float mm = row_max(m), mv = row_max(v);
                 uint32_t qm = 0, qv = 0;
-                if (mm >= kDead && mm <= 3.402823466e38f) {
-                    float y[4];
-                    uint32_t w[4];
-                    scaled_row(m, mm, y);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = round_q8(y[j], bits[j] & 0xfffffu);
-                    qm = top_bytes(w);
-                }
-                if (mv >= kDead && mv <= 3.402823466e38f) {
-                    float y[4];
-                    uint32_t w[4];
-                    scaled_row(v, mv, y);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = max((__float_as_uint(y[j]) + (bits[j] >> 12)) << 4, v[j] > 0.f ? 1u << 24 : 0u);
-                    qv = top_bytes(w);
+                float em = mm * (1.f / 448.f), ev = mv * (1.f / 448.f);
+                if (usual(mm) && usual(mv)) {
+                    qm = codes(m, codes_per_unit(mm), 1.f, bits);
+                    qv = codes_positive(v, codes_per_unit(mv), 1.f, bits);
+                } else {
+                    const float lm = usual(mm) ? 1.f : 0x1p-114f, lv = usual(mv) ? 1.f : 0x1p-114f;
+                    if (held(mm)) qm = codes(m, codes_per_unit(mm * lm), lm, bits);
+                    if (held(mv)) qv = codes_positive(v, codes_per_unit(mv * lv), lv, bits);
+                    em = scale_of(mm);
+                    ev = scale_of(mv);
                 }
                 store_b8<WHOLE>(pm, i, n, qm);
                 store_b8<WHOLE>(pv, i, n, qv);
                 if (lane == 0 && (WHOLE || i < n)) {
-                    pms[r] = scale_of(mm);
-                    pvs[r] = scale_of(mv);
+                    pms[r] = em;
+                    pvs[r] = ev;
                 }
             }
         }
+        if (Q8 && WHOLE) raw = next;
         pg += kChunk * kG;
         pp += kChunk * kP;
         pm += kChunk * kS;
@@ -429,17 +450,10 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
         if (pc) pc += kChunk * 2;
         if (Q8) { pms += kChunk / kRow; pvs += kChunk / kRow; }
         row0 += kChunk / kRow;
-        n -= kChunk;
     }
 }
 
-template <bool Q8, bool PB, bool GB>
-__device__ __forceinline__ void update_share(const Tensor& t, const Coefficients& k, const Share& s, int lane) {
-    if (s.whole) update<Q8, PB, GB, true>(t, k, s.first, s.whole, lane);
-    if (s.rest) update<Q8, PB, GB, false>(t, k, s.first + s.whole * (long long)kChunk, 1, lane);
-}
-
-template <int MANY, bool Q8>
+template <int MANY, bool Q8, bool PB, bool GB>
 __global__ void __launch_bounds__(kThreads, 4) step_kernel(const __grid_constant__ Args<MANY> a) {
     __shared__ double scratch[kWarps];
     __shared__ float hyper[2];
@@ -469,8 +483,8 @@ __global__ void __launch_bounds__(kThreads, 4) step_kernel(const __grid_constant
         at = tensor_of(a, c, at);
         const Tensor& t = a.t[at];
         const Share s(t, c, a.span, warp, lane);
-        if (t.p_bf16) t.g_bf16 ? update_share<Q8, true, true>(t, k, s, lane) : update_share<Q8, true, false>(t, k, s, lane);
-        else t.g_bf16 ? update_share<Q8, false, true>(t, k, s, lane) : update_share<Q8, false, false>(t, k, s, lane);
+        if (s.whole) update<Q8, PB, GB, true>(t, k, s.begin, s.own, s.whole, 0, lane);
+        if (s.rest) update<Q8, PB, GB, false>(t, k, s.begin + s.whole * kChunk, s.own, 1, s.rest, lane);
     }
 }
 
@@ -547,10 +561,17 @@ void fill(adamw::Args<MANY>& a, const hla_adamw* c, int from, int n) {
     }
 }
 
-// Tensors from `from` on that one launch takes.
+// Tensors from `from` on that one launch takes: of the same types.
 int batch(const hla_adamw* c, int from) {
-    const int left = (int)c->t.size() - from;
-    return left < adamw::kMany ? left : adamw::kMany;
+    int n = 1;
+    while (from + n < (int)c->t.size() && n < adamw::kMany && c->t[from + n].p_bf16 == c->t[from].p_bf16 && c->t[from + n].g_bf16 == c->t[from].g_bf16) ++n;
+    return n;
+}
+
+template <int MANY, bool Q8>
+void (*step_of(const adamw::Tensor& t))(adamw::Args<MANY>) {
+    if (t.p_bf16) return t.g_bf16 ? adamw::step_kernel<MANY, Q8, true, true> : adamw::step_kernel<MANY, Q8, true, false>;
+    return t.g_bf16 ? adamw::step_kernel<MANY, Q8, false, true> : adamw::step_kernel<MANY, Q8, false, false>;
 }
 
 int norm_blocks(const hla_adamw* c, uint32_t units) { return (int)std::min<uint32_t>(units, 8u * c->sm_count); }
@@ -589,7 +610,8 @@ hla_status step(const hla_adamw* c, const hla_adamw_step_args& s, double* part, 
             fill(a, c, from, batch(c, from));
             const int blocks = norm_blocks(c, a.units);
             a.part = part + a.norm_blocks;
-            adamw::norm_kernel<MANY><<<blocks, adamw::kThreads, 0, st>>>(a);
+            if (c->t[from].g_bf16) adamw::norm_kernel<MANY, true><<<blocks, adamw::kThreads, 0, st>>>(a);
+            else adamw::norm_kernel<MANY, false><<<blocks, adamw::kThreads, 0, st>>>(a);
             if (cudaGetLastError() != cudaSuccess) return HLA_ERR_CUDA;
             a.norm_blocks += blocks;
         }
@@ -599,8 +621,7 @@ hla_status step(const hla_adamw* c, const hla_adamw_step_args& s, double* part, 
         fill(a, c, from, batch(c, from));
         if (from) a.norm_out = nullptr;
         const dim3 blocks(std::min<uint32_t>(a.units, 4u * c->sm_count));
-        const bool ok = k.state == HLA_STATE_Q8 ? launch_step(adamw::step_kernel<MANY, true>, blocks, a, st) : launch_step(adamw::step_kernel<MANY, false>, blocks, a, st);
-        if (!ok) return HLA_ERR_CUDA;
+        if (!launch_step(k.state == HLA_STATE_Q8 ? step_of<MANY, true>(c->t[from]) : step_of<MANY, false>(c->t[from]), blocks, a, st)) return HLA_ERR_CUDA;
     }
     return HLA_OK;
 }
@@ -647,6 +668,7 @@ hla_status hla_adamw_create(const hla_adamw_config* cfg, const hla_adamw_tensor*
             d.g_bf16 = t.grad_dtype == HLA_BF16;
             c->t.push_back(d);
         }
+        std::stable_sort(c->t.begin(), c->t.end(), [](const adamw::Tensor& a, const adamw::Tensor& b) { return 2 * a.p_bf16 + a.g_bf16 < 2 * b.p_bf16 + b.g_bf16; });
         if (st == HLA_OK && chunks >= (1ull << 31)) st = HLA_ERR_UNSUPPORTED;
         if (st == HLA_OK) st = check_spans(c.get());
         if (st == HLA_OK) *out = c.release();
