@@ -127,13 +127,18 @@ __device__ __forceinline__ uint4 load_any(const void* base, int i, int n) {
     return make_uint4(r.x, r.y, 0, 0);
 }
 template <bool BF16>
-__device__ __forceinline__ void unpack(const uint4& r, float (&x)[4]) {
+__device__ __forceinline__ void unpack(const uint4& r, P2 (&x)[2]) {
     if (BF16) {
-        x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xffff0000u);
-        x[2] = __uint_as_float(r.y << 16); x[3] = __uint_as_float(r.y & 0xffff0000u);
+        x[0] = pair(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u));
+        x[1] = pair(__uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
     } else {
-        x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+        x[0] = pair(__uint_as_float(r.x), __uint_as_float(r.y));
+        x[1] = pair(__uint_as_float(r.z), __uint_as_float(r.w));
     }
+}
+__device__ __forceinline__ void four(const P2 (&x)[2], float (&y)[4]) {
+    const float2 a = both(x[0]), b = both(x[1]);
+    y[0] = a.x; y[1] = a.y; y[2] = b.x; y[3] = b.y;
 }
 template <bool WHOLE>
 __device__ __forceinline__ void store_f32(void* base, int i, int n, const float (&x)[4]) {
@@ -164,12 +169,11 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
 }
 
 // Two e4m3 codes as floats (exact).
-__device__ __forceinline__ void decode2(uint32_t codes, float& x, float& y) {
+__device__ __forceinline__ P2 decode2(uint32_t codes) {
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)codes));
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    x = f.x;
-    y = f.y;
+    return pair(f.x, f.y);
 }
 
 __device__ __forceinline__ float max_abs(float a, float b, float c) {      // a NaN stays
@@ -191,7 +195,9 @@ __device__ __forceinline__ float reciprocal(float x) {
 }
 
 // The largest of a row's |x| from every lane's own four; not a number if one of them is none.
-__device__ __forceinline__ float row_max(const float (&x)[4]) {
+__device__ __forceinline__ float row_max(const P2 (&v)[2]) {
+    float x[4];
+    four(v, x);
     const float most = max_abs(max_abs(x[0], x[1], x[2]), x[3], x[3]);
     return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));      // (bits of non-negative floats are ordered like them)
 }
@@ -207,16 +213,24 @@ __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&w)[4]) {
 }
 // The codes of four entries, of a moment that may be negative (low random bits) and of one that may not (high ones, and at least 1 where
 // the entry is not zero).
-__device__ __forceinline__ uint32_t codes(const float (&x)[4], float per, float less, const uint32_t (&bits)[4]) {
+__device__ __forceinline__ uint32_t codes(const P2 (&x)[2], float per, float less, const uint32_t (&bits)[4]) {
+    const P2 scaled[2] = {less == 1.f ? mul2(x[0], twice(per)) : mul2(mul2(x[0], twice(less)), twice(per)), less == 1.f ? mul2(x[1], twice(per)) : mul2(mul2(x[1], twice(less)), twice(per))};
+    float y[4], s[4];
+    four(scaled, y);
+    four(x, s);
     uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = (__float_as_uint(fabsf(x[j]) * less * per) * 16u + (bits[j] * 4096u >> 8)) | (__float_as_uint(x[j]) & 0x80000000u);
+    for (int j = 0; j < 4; ++j) w[j] = (__float_as_uint(y[j]) * 16u + (bits[j] * 4096u >> 8)) | (__float_as_uint(s[j]) & 0x80000000u);      // (the sign is shifted out)
     return top_bytes(w);
 }
-__device__ __forceinline__ uint32_t codes_positive(const float (&x)[4], float per, float less, const uint32_t (&bits)[4]) {
+__device__ __forceinline__ uint32_t codes_positive(const P2 (&x)[2], float per, float less, const uint32_t (&bits)[4]) {
+    const P2 scaled[2] = {less == 1.f ? mul2(x[0], twice(per)) : mul2(mul2(x[0], twice(less)), twice(per)), less == 1.f ? mul2(x[1], twice(per)) : mul2(mul2(x[1], twice(less)), twice(per))};
+    float y[4], s[4];
+    four(scaled, y);
+    four(x, s);
     uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = max(__float_as_uint(x[j] * less * per), min(__float_as_uint(x[j]), 1u << 20)) * 16u + (bits[j] >> 8);
+    for (int j = 0; j < 4; ++j) w[j] = max(__float_as_uint(y[j]), min(__float_as_uint(s[j]), 1u << 20)) * 16u + (bits[j] >> 8);
     return top_bytes(w);
 }
 // Rows whose factor would not be a normal number (their largest entry from 2^14 on) are made smaller first.
@@ -277,8 +291,10 @@ __device__ __forceinline__ double run_squares(const char* base, int own, int cou
         for (int r = 0; r < kRows; ++r) raw[r] = load_any<BF16, WHOLE>(base, r * kRow, n - own);
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
+            P2 pairs[2];
             float g[4];
-            unpack<BF16>(raw[r], g);
+            unpack<BF16>(raw[r], pairs);
+            four(pairs, g);
             sum += squares(g);
         }
     }
@@ -339,7 +355,8 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
     if (pc) pc += own * 2;
     if (Q8) { pms += own / kRow; pvs += own / kRow; }
     n -= own;
-    // the chunk that is `ahead` (0 or 1) chunks from here
+    uint32_t row0 = row_first + own / kRow;
+    // the chunk that is `ahead` chunks from here
     auto load = [&](Raw& x, int ahead) {
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
@@ -358,23 +375,17 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
             }
         }
     };
-    // 8-bit states: the next chunk is on its way during the arithmetic of this one, which takes as long as its bytes
-    Raw raw, next;
-    if (Q8) load(raw, 0);
-    uint32_t row0 = row_first + own / kRow;
-    for (; count > 0; --count) {
-        if (!Q8) load(raw, 0);
-        else if (WHOLE && count > 1) load(next, 1);
+    auto compute = [&](const Raw& raw, int ahead) {
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            const int i = r * kRow;
-            float g[4], p[4], m[4], v[4];
+            const int i = ahead * kChunk + r * kRow;
+            P2 g[2], m[2], v[2], w[2];
             unpack<GB>(raw.g[r], g);
-            unpack<PB>(raw.p[r], p);
+            unpack<PB>(raw.p[r], w);
             float cb1 = k.b1, cb2 = k.b2;
             if (Q8) {
-                decode2(raw.cm[r], m[0], m[1]); decode2(raw.cm[r] >> 16, m[2], m[3]);
-                decode2(raw.cv[r], v[0], v[1]); decode2(raw.cv[r] >> 16, v[2], v[3]);
+                m[0] = decode2(raw.cm[r]); m[1] = decode2(raw.cm[r] >> 16);
+                v[0] = decode2(raw.cv[r]); v[1] = decode2(raw.cv[r] >> 16);
                 cb1 *= raw.sm[r];
                 cb2 *= raw.sv[r];
             } else {
@@ -382,15 +393,20 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
                 unpack<false>(raw.v[r], v);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                g[j] *= k.gain;
-                m[j] = fmaf(k.r1, g[j], cb1 * m[j]);
-                v[j] = fmaf(k.r2 * g[j], g[j], cb2 * v[j]);
-                p[j] = fmaf(-size, m[j] * reciprocal(fmaf(sqrt_fast(v[j]), k.inv2, k.eps)), fmaf(-shrink, p[j], p[j]));
+            for (int j = 0; j < 2; ++j) {
+                g[j] = mul2(g[j], twice(k.gain));
+                m[j] = fma2(twice(k.r1), g[j], mul2(twice(cb1), m[j]));
+                v[j] = fma2(mul2(twice(k.r2), g[j]), g[j], mul2(twice(cb2), v[j]));
+                const float2 square = both(v[j]);
+                const float2 below = both(fma2(pair(sqrt_fast(square.x), sqrt_fast(square.y)), twice(k.inv2), twice(k.eps)));
+                const P2 quotient = mul2(m[j], pair(reciprocal(below.x), reciprocal(below.y)));
+                w[j] = fma2(twice(-size), quotient, fma2(twice(-shrink), w[j], w[j]));
             }
+            float p[4];
+            four(w, p);
             uint32_t bits[4];
             if (Q8 || PB) {
-                const uint32_t block = mix32(tensor_key + (row0 + r) * 0x9E3779B9u) + (uint32_t)lane * 2u * 0x9E3779B9u;
+                const uint32_t block = mix32(tensor_key + (row0 + ahead * (kChunk / kRow) + r) * 0x9E3779B9u) + (uint32_t)lane * 2u * 0x9E3779B9u;
 #pragma unroll
                 for (int j = 0; j < 4; j += 2) {
                     uint32_t x = block + (uint32_t)(j / 2) * 0x9E3779B9u;
@@ -418,8 +434,11 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
                 if (pc) store_bf16<WHOLE>(pc, i, n, two_bf16(p[0], p[1]), two_bf16(p[2], p[3]));
             }
             if (!Q8) {
-                store_f32<WHOLE>(pm, i, n, m);
-                store_f32<WHOLE>(pv, i, n, v);
+                float x[4], y[4];
+                four(m, x);
+                four(v, y);
+                store_f32<WHOLE>(pm, i, n, x);
+                store_f32<WHOLE>(pv, i, n, y);
             } else {
                 const float mm = row_max(m), mv = row_max(v);
                 uint32_t qm = 0, qv = 0;
@@ -437,19 +456,40 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
                 store_b8<WHOLE>(pm, i, n, qm);
                 store_b8<WHOLE>(pv, i, n, qv);
                 if (lane == 0 && (WHOLE || i < n)) {
-                    pms[r] = em;
-                    pvs[r] = ev;
+                    pms[i / kRow] = em;
+                    pvs[i / kRow] = ev;
                 }
             }
         }
-        if (Q8 && WHOLE) raw = next;
-        pg += kChunk * kG;
-        pp += kChunk * kP;
-        pm += kChunk * kS;
-        pv += kChunk * kS;
-        if (pc) pc += kChunk * 2;
-        if (Q8) { pms += kChunk / kRow; pvs += kChunk / kRow; }
-        row0 += kChunk / kRow;
+    };
+    auto advance = [&](int chunks) {
+        pg += chunks * kChunk * kG;
+        pp += chunks * kChunk * kP;
+        pm += chunks * kChunk * kS;
+        pv += chunks * kChunk * kS;
+        if (pc) pc += chunks * kChunk * 2;
+        if (Q8) { pms += chunks * (kChunk / kRow); pvs += chunks * (kChunk / kRow); }
+        row0 += chunks * (kChunk / kRow);
+    };
+    Raw x;
+    if (Q8 && WHOLE) {      // the next chunk is on its way during the arithmetic of this one, which takes as long as its bytes
+        Raw y;
+        load(x, 0);
+        for (; count > 0; count -= 2) {
+            if (count > 1) load(y, 1);
+            compute(x, 0);
+            if (count > 1) {
+                if (count > 2) load(x, 2);
+                compute(y, 1);
+            }
+            advance(2);
+        }
+    } else {
+        for (; count > 0; --count) {
+            load(x, 0);
+            compute(x, 0);
+            advance(1);
+        }
     }
 }
 

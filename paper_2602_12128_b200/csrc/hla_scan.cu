@@ -54,14 +54,6 @@ __device__ __forceinline__ uint32_t of_block(uint32_t local, uint32_t rank) {
     return r;
 }
 
-// ---- two channels in one register pair -------------------------------------------------------------------------------------
-using P2 = unsigned long long;
-__device__ __forceinline__ P2 pair(float x, float y) { P2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y)); return r; }
-__device__ __forceinline__ float2 both(P2 v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
-__device__ __forceinline__ P2 fma2(P2 a, P2 b, P2 c) { P2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ P2 mul2(P2 a, P2 b) { P2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ P2 add2(P2 a, P2 b) { P2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ P2 twice(float x) { return pair(x, x); }
 __device__ __forceinline__ P2 one_minus(P2 x) { return fma2(x, twice(-1.f), twice(1.f)); }
 
 __device__ __forceinline__ float exp2_fast(float x) {
