@@ -23,6 +23,7 @@ namespace heads {
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = kMaxD / 2;
 constexpr int kDwThreads = 1024;
+constexpr int kStages = 4;          // rows of a group on their way in the backward
 
 struct Tensor {
     const char *x, *dy;          // projection (strided); gradient of the prepared tensor (head-major)
@@ -50,39 +51,42 @@ struct Args {
     int want_dw;
 };
 
-// 16 bytes of a row as NP pairs of fp32.  Adjacent pairing: 16 consecutive bytes; half-split: 8 bytes at either place.
+// 16 bytes of a row as fp32: the first and the second channels of its NP pairs, two pairs in a register pair (rotation, norm and their
+// gradients are then single instructions for two pairs).  Adjacent pairing: 16 consecutive bytes; half-split: 8 bytes at either place.
 template <typename T, bool HALF> struct Vec;
 template <bool HALF> struct Vec<__nv_bfloat16, HALF> {
-    static constexpr int CH = 8, NP = 4;
-    static __device__ __forceinline__ void unpack(const uint4& r, float (&a)[4], float (&b)[4]) {
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xffff0000u);
-            if (!HALF) { a[i] = lo; b[i] = hi; }
-            else if (i < 2) { a[2 * i] = lo; a[2 * i + 1] = hi; }
-            else { b[2 * i - 4] = lo; b[2 * i - 3] = hi; }
+    static constexpr int CH = 8, NP = 4, NQ = 2;
+    static __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
+    static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+    static __device__ __forceinline__ void unpack(const uint4& r, P2 (&a)[2], P2 (&b)[2]) {
+        if (HALF) {
+            a[0] = pair(lo(r.x), hi(r.x)); a[1] = pair(lo(r.y), hi(r.y));
+            b[0] = pair(lo(r.z), hi(r.z)); b[1] = pair(lo(r.w), hi(r.w));
+        } else {
+            a[0] = pair(lo(r.x), lo(r.y)); a[1] = pair(lo(r.z), lo(r.w));
+            b[0] = pair(hi(r.x), hi(r.y)); b[1] = pair(hi(r.z), hi(r.w));
         }
     }
-    static __device__ __forceinline__ uint32_t two(float lo, float hi) {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    static __device__ __forceinline__ uint32_t two(float x, float y) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
         return *reinterpret_cast<const uint32_t*>(&v);
     }
-    static __device__ __forceinline__ uint4 pack(const float (&a)[4], const float (&b)[4]) {
-        if (!HALF) return make_uint4(two(a[0], b[0]), two(a[1], b[1]), two(a[2], b[2]), two(a[3], b[3]));
-        return make_uint4(two(a[0], a[1]), two(a[2], a[3]), two(b[0], b[1]), two(b[2], b[3]));
+    static __device__ __forceinline__ uint4 pack(const P2 (&pa)[2], const P2 (&pb)[2]) {
+        const float2 a0 = both(pa[0]), a1 = both(pa[1]), b0 = both(pb[0]), b1 = both(pb[1]);
+        if (HALF) return make_uint4(two(a0.x, a0.y), two(a1.x, a1.y), two(b0.x, b0.y), two(b1.x, b1.y));
+        return make_uint4(two(a0.x, b0.x), two(a0.y, b0.y), two(a1.x, b1.x), two(a1.y, b1.y));
     }
 };
 template <bool HALF> struct Vec<float, HALF> {
-    static constexpr int CH = 4, NP = 2;
-    static __device__ __forceinline__ void unpack(const uint4& r, float (&a)[2], float (&b)[2]) {
-        a[0] = __uint_as_float(r.x);
-        (HALF ? a[1] : b[0]) = __uint_as_float(r.y);
-        (HALF ? b[0] : a[1]) = __uint_as_float(r.z);
-        b[1] = __uint_as_float(r.w);
+    static constexpr int CH = 4, NP = 2, NQ = 1;
+    static __device__ __forceinline__ void unpack(const uint4& r, P2 (&a)[1], P2 (&b)[1]) {
+        const float x = __uint_as_float(r.x), y = __uint_as_float(r.y), z = __uint_as_float(r.z), w = __uint_as_float(r.w);
+        a[0] = HALF ? pair(x, y) : pair(x, z);
+        b[0] = HALF ? pair(z, w) : pair(y, w);
     }
-    static __device__ __forceinline__ uint4 pack(const float (&a)[2], const float (&b)[2]) {
-        return make_uint4(__float_as_uint(a[0]), __float_as_uint(HALF ? a[1] : b[0]), __float_as_uint(HALF ? b[0] : a[1]), __float_as_uint(b[1]));
+    static __device__ __forceinline__ uint4 pack(const P2 (&pa)[1], const P2 (&pb)[1]) {
+        const float2 a = both(pa[0]), b = both(pb[0]);
+        return make_uint4(__float_as_uint(a.x), __float_as_uint(HALF ? a.y : b.x), __float_as_uint(HALF ? b.x : a.y), __float_as_uint(b.y));
     }
 };
 
@@ -112,6 +116,16 @@ struct Place {
         }
         return r;
     }
+    // Asynchronously into shared memory, both places next to one another.
+    __device__ __forceinline__ void copy(uint4* to, const char* row) const {
+        const uint32_t a = (uint32_t)__cvta_generic_to_shared(to);
+        if (HALF) {
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(a), "l"(row + off_a) : "memory");
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(a + 8), "l"(row + off_b) : "memory");
+        } else {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(a), "l"(row + off_a) : "memory");
+        }
+    }
     __device__ __forceinline__ void store(char* row, const uint4& r) const {
         if (HALF) {
             *reinterpret_cast<uint2*>(row + off_a) = make_uint2(r.x, r.y);
@@ -125,199 +139,283 @@ struct Place {
 // cos and sin of a lane's pairs at token n of batch b, times `scale`.  The angle is reduced to a fraction of a turn in 64 bits: at
 // position 2^31 its error is below 2^-22 turns.
 template <typename T, bool HALF>
-__device__ __forceinline__ void angles(const Args& p, const double* turns, int l, int b, int n, float scale, float (&c)[Vec<T, HALF>::NP], float (&s)[Vec<T, HALF>::NP]) {
+__device__ __forceinline__ void angles(const Args& p, const double* turns, int l, int b, int n, float scale, P2 (&c)[Vec<T, HALF>::NQ], P2 (&s)[Vec<T, HALF>::NQ]) {
     constexpr int NP = Vec<T, HALF>::NP;
     int pos[3] = {0, 0, 0};
 #pragma unroll
     for (int a = 0; a < 3; ++a)
         if (a < p.n_axes) pos[a] = p.positions ? p.positions[b * p.pos_batch + (long long)n * p.n_axes + a] : n / p.stride[a] % p.grid[a] + p.start[a];
+    float cs[NP], sn[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        const int pair = l * NP + i;
-        c[i] = scale;
-        s[i] = 0.f;
-        if (pair < p.pair_end[2]) {
-            const double x = (double)(pair < p.pair_end[0] ? pos[0] : pair < p.pair_end[1] ? pos[1] : pos[2]) * turns[pair];
-            float sn, cs;
-            sincospif(2.f * (float)(x - rint(x)), &sn, &cs);
-            c[i] = cs * scale;
-            s[i] = sn * scale;
+        const int pair_ = l * NP + i;
+        cs[i] = 1.f;
+        sn[i] = 0.f;
+        if (pair_ < p.pair_end[2]) {
+            const double x = (double)(pair_ < p.pair_end[0] ? pos[0] : pair_ < p.pair_end[1] ? pos[1] : pos[2]) * turns[pair_];
+            sincospif(2.f * (float)(x - rint(x)), &sn[i], &cs[i]);
         }
+    }
+#pragma unroll
+    for (int i = 0; i < NP / 2; ++i) {
+        c[i] = pair(cs[2 * i] * scale, cs[2 * i + 1] * scale);
+        s[i] = pair(sn[2 * i] * scale, sn[2 * i + 1] * scale);
     }
 }
 
-__device__ __forceinline__ float lanes_sum(float v, int log_lanes) {
-    for (int o = 1 << log_lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+// Sums over the lanes of a row of U values at once.  LOG: the lanes' number where it is known to the compiler (a loop costs as much as the
+// shuffles), 0 else.
+template <int LOG, int U>
+__device__ __forceinline__ void lanes_sum(float (&v)[U], int log_lanes) {
+    if (LOG) {
+#pragma unroll
+        for (int o = 1 << LOG >> 1; o > 0; o >>= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] += __shfl_xor_sync(0xffffffffu, v[u], o);
+    } else {
+        for (int o = 1 << log_lanes >> 1; o > 0; o >>= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] += __shfl_xor_sync(0xffffffffu, v[u], o);
+    }
 }
 
-template <typename T, bool HALF, bool NORM>
-__global__ void __launch_bounds__(kThreads) forward_kernel(const __grid_constant__ Args p) {
+template <typename T, bool HALF>
+__device__ __forceinline__ void norm_weights(const void* w, const Place<T, HALF>& at, P2 (&wa)[Vec<T, HALF>::NQ], P2 (&wb)[Vec<T, HALF>::NQ]) {
+    if (w) {
+        uint4 r = make_uint4(0, 0, 0, 0);
+        if (at.in) r = at.load(static_cast<const char*>(w));
+        Vec<T, HALF>::unpack(r, wa, wb);
+    } else {
+#pragma unroll
+        for (int i = 0; i < Vec<T, HALF>::NQ; ++i) wa[i] = wb[i] = twice(1.f);
+    }
+}
+
+template <typename T, bool HALF, bool NORM, int LOG>
+__global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_constant__ Args p) {
     using V = Vec<T, HALF>;
-    constexpr int NP = V::NP, U = 4;
+    constexpr int NQ = V::NQ, U = 4;
     __shared__ double turns[kMaxPairs];
     if (threadIdx.x < kMaxPairs) turns[threadIdx.x] = p.turns[threadIdx.x];
     __syncthreads();
-    const int l = threadIdx.x & ((1 << p.log_lanes) - 1);
+    const int log_lanes = LOG ? LOG : p.log_lanes;
+    const int l = threadIdx.x & ((1 << log_lanes) - 1);
     const uint32_t tokens = (uint32_t)p.B * p.N, units = tokens * p.n_tensors * p.chunks;
-    uint32_t unit = blockIdx.x * (uint32_t)(kThreads >> p.log_lanes) + (threadIdx.x >> p.log_lanes);
+    uint32_t unit = blockIdx.x * (uint32_t)(kThreads >> log_lanes) + (threadIdx.x >> log_lanes);
     const bool live = unit < units;
     if (!live) unit = 0;      // (stays for the shuffles of its warp)
     const uint32_t run = unit / tokens, token = unit - run * tokens;
     const int b = token / p.N, n = token - b * p.N;
     const Tensor& t = p.t[run / p.chunks];
-    const int h0 = (run % p.chunks) * p.per_chunk, h1 = min(p.H, h0 + p.per_chunk);
+    const int h0 = (run % p.chunks) * p.per_chunk, count = min(p.H - h0, p.per_chunk);
     const Place<T, HALF> at(p, l);
     const bool mine = live && at.in;
     const size_t row = (size_t)p.d * sizeof(T), head = row * p.N;
     const char* src = t.x + b * t.x_batch + n * t.x_token + h0 * row;
     char* dst = t.out + ((size_t)b * p.H + h0) * head + n * row;
 
-    float c[NP], s[NP], wa[NP], wb[NP];
+    P2 c[NQ], s[NQ], wa[NQ], wb[NQ];
     if (t.rotate) {
         angles<T, HALF>(p, turns, l, b, n, t.scale, c, s);
-        if (NORM) {
-            uint4 w = {};
-            if (t.w && mine) { w = at.load(static_cast<const char*>(t.w)); }
-            V::unpack(w, wa, wb);
-            if (!t.w) {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) wa[i] = wb[i] = 1.f;
-            }
-        }
+        if (NORM) norm_weights<T, HALF>(t.w, at, wa, wb);
     }
     for (int h = 0; h < p.per_chunk; h += U) {
         uint4 r[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             r[u] = make_uint4(0, 0, 0, 0);
-            if (mine && h0 + h + u < h1) r[u] = at.load(src + (h + u) * row);
+            if (mine && h + u < count) r[u] = at.load(src + u * row);
         }
+        if (t.rotate) {
+            float scale[U];
+            if (NORM) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (h + u >= p.per_chunk) break;
-            if (t.rotate) {
-                float a[NP], v[NP];
-                V::unpack(r[u], a, v);
-                if (NORM) {
-                    float ss = 0.f;
+                for (int u = 0; u < U; ++u) {
+                    P2 x[NQ], y[NQ];
+                    V::unpack(r[u], x, y);
+                    P2 sum = mul2(x[0], x[0]);
 #pragma unroll
-                    for (int i = 0; i < NP; ++i) ss += a[i] * a[i] + v[i] * v[i];
-                    const float q = rsqrtf(lanes_sum(ss, p.log_lanes) * p.inv_d + p.eps);
+                    for (int i = 1; i < NQ; ++i) sum = fma2(x[i], x[i], sum);
 #pragma unroll
-                    for (int i = 0; i < NP; ++i) { a[i] = a[i] * q * wa[i]; v[i] = v[i] * q * wb[i]; }
+                    for (int i = 0; i < NQ; ++i) sum = fma2(y[i], y[i], sum);
+                    const float2 f = both(sum);
+                    scale[u] = f.x + f.y;
                 }
-                float ya[NP], yb[NP];
+                lanes_sum<LOG, U>(scale, log_lanes);
+            }
 #pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    ya[i] = a[i] * c[i] - v[i] * s[i];
-                    yb[i] = a[i] * s[i] + v[i] * c[i];
+            for (int u = 0; u < U; ++u) {
+                P2 x[NQ], y[NQ];
+                V::unpack(r[u], x, y);
+                if (NORM) {
+                    const P2 q = twice(rsqrtf(fmaf(scale[u], p.inv_d, p.eps)));
+#pragma unroll
+                    for (int i = 0; i < NQ; ++i) {
+                        x[i] = mul2(mul2(x[i], q), wa[i]);
+                        y[i] = mul2(mul2(y[i], q), wb[i]);
+                    }
+                }
+                P2 ya[NQ], yb[NQ];
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) {
+                    ya[i] = fma2(x[i], c[i], neg2(mul2(y[i], s[i])));
+                    yb[i] = fma2(x[i], s[i], mul2(y[i], c[i]));
                 }
                 r[u] = V::pack(ya, yb);
             }
-            if (mine && h0 + h + u < h1) at.store(dst + (size_t)(h + u) * head, r[u]);
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (mine && h + u < count) at.store(dst + u * head, r[u]);
+        src += U * row;
+        dst += U * head;
     }
 }
 
+// The rows of a block's tokens one after the other: token tiles outside, the heads of its run inside.  Every group of lanes walks its own.
+template <typename T, bool HALF>
+struct Walk {
+    const Args& p;
+    const Tensor& t;
+    uint32_t first;           // token of the block's first group
+    int group, h, h0, count;
+    bool in, mine;
+    const char *dy, *x;
+    __device__ __forceinline__ Walk(const Args& a, const Tensor& tensor, int g, int h0_, int count_, bool in_) : p(a), t(tensor), first(0), group(g), h(0), h0(h0_), count(count_), in(in_) {}
+    __device__ __forceinline__ void tile(uint32_t at, int groups, uint32_t tokens, int& b, int& n) {
+        first = at;
+        h = 0;
+        const bool live = first + group < tokens;
+        mine = live && in;
+        const uint32_t token = live ? first + group : first;
+        b = token / p.N;
+        n = token - b * p.N;
+    }
+    __device__ __forceinline__ void pointers(int b, int n, size_t row) {
+        dy = t.dy + (((size_t)b * p.H + h0) * p.N + n) * row;
+        x = t.x + b * t.x_batch + n * t.x_token + h0 * row;
+    }
+};
+
 // A block stays with one run of heads of one tensor (blockIdx.y) and goes through tokens, so that its sums for the weight gradient
-// can stay in registers until the end.
-template <typename T, bool HALF, bool NORM>
-__global__ void __launch_bounds__(kThreads) backward_kernel(const __grid_constant__ Args p) {
+// can stay in registers until the end.  Rows come kStages ahead through shared memory, every lane its own 16 bytes (registers for as many
+// rows in flight are not there): with two rows of registers ahead the backward of 2 x 24 x 32760 rows took 660 us.
+template <typename T, bool HALF, bool NORM, int LOG>
+__global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_constant__ Args p) {
     using V = Vec<T, HALF>;
-    constexpr int NP = V::NP, U = 2;
+    constexpr int NP = V::NP, NQ = V::NQ;
     __shared__ double turns[kMaxPairs];
     __shared__ float sums[kThreads * 2 * NP];
+    __shared__ uint4 staged[kStages][NORM ? 2 : 1][kThreads];
     if (threadIdx.x < kMaxPairs) turns[threadIdx.x] = p.turns[threadIdx.x];
     __syncthreads();
-    const int l = threadIdx.x & ((1 << p.log_lanes) - 1), groups = kThreads >> p.log_lanes, group = threadIdx.x >> p.log_lanes;
+    const int log_lanes = LOG ? LOG : p.log_lanes;
+    const int l = threadIdx.x & ((1 << log_lanes) - 1), groups = kThreads >> log_lanes, group = threadIdx.x >> log_lanes;
     const int ti = blockIdx.y / p.chunks, chunk = blockIdx.y % p.chunks;
     const Tensor& t = p.t[ti];
-    const int h0 = chunk * p.per_chunk, h1 = min(p.H, h0 + p.per_chunk);
+    const int h0 = chunk * p.per_chunk, count = min(p.H - h0, p.per_chunk);
     const Place<T, HALF> at(p, l);
     const size_t row = (size_t)p.d * sizeof(T), head = row * p.N;
-    const uint32_t tokens = (uint32_t)p.B * p.N;
-    float wa[NP], wb[NP], da[NP], db[NP];
+    const uint32_t tokens = (uint32_t)p.B * p.N, stride = gridDim.x * groups;
+    const bool rotate = t.rotate;
+    P2 wa[NQ], wb[NQ], da[NQ], db[NQ];
 #pragma unroll
-    for (int i = 0; i < NP; ++i) { wa[i] = wb[i] = 1.f; da[i] = db[i] = 0.f; }
-    if (NORM && t.rotate && t.w) {
-        uint4 w = {};
-        if (at.in) w = at.load(static_cast<const char*>(t.w));
-        V::unpack(w, wa, wb);
-    }
-    for (uint32_t first = blockIdx.x * groups; first < tokens; first += gridDim.x * groups) {
+    for (int i = 0; i < NQ; ++i) da[i] = db[i] = 0;
+    if (NORM && rotate) norm_weights<T, HALF>(t.w, at, wa, wb);
+
+    Walk<T, HALF> ahead(p, t, group, h0, count, at.in);
+    int ab, an;
+    ahead.tile(blockIdx.x * groups, groups, tokens, ab, an);
+    ahead.pointers(ab, an, row);
+    auto fetch = [&](int stage) {
+        if (ahead.first < tokens) {
+            if (ahead.mine) {
+                at.copy(&staged[stage][0][threadIdx.x], ahead.dy);
+                if (NORM && rotate) at.copy(&staged[stage][NORM ? 1 : 0][threadIdx.x], ahead.x);
+            }
+            ahead.dy += head;
+            ahead.x += row;
+            if (++ahead.h == count) {
+                ahead.tile(ahead.first + stride, groups, tokens, ab, an);
+                if (ahead.first < tokens) ahead.pointers(ab, an, row);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) fetch(i);
+    int stage = 0;
+    for (uint32_t first = blockIdx.x * groups; first < tokens; first += stride) {
         const bool live = first + group < tokens;
         const uint32_t token = live ? first + group : first;
         const int b = token / p.N, n = token - b * p.N;
         const bool mine = live && at.in;
-        const char* dy = t.dy + ((size_t)b * p.H + h0) * head + n * row;
-        const char* src = t.x + b * t.x_batch + n * t.x_token + h0 * row;
         char* dst = t.out + b * t.o_batch + n * t.o_token + h0 * row;
-        float c[NP], s[NP];
-        if (t.rotate) angles<T, HALF>(p, turns, l, b, n, t.scale, c, s);
-        for (int h = 0; h < p.per_chunk; h += U) {
-            uint4 r[U], x[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                r[u] = x[u] = make_uint4(0, 0, 0, 0);
-                if (mine && h0 + h + u < h1) {
-                    r[u] = at.load(dy + (size_t)(h + u) * head);
-                    if (NORM && t.rotate) x[u] = at.load(src + (h + u) * row);
-                }
+        P2 c[NQ], s[NQ];
+        if (rotate) angles<T, HALF>(p, turns, l, b, n, t.scale, c, s);
+        for (int h = 0; h < count; ++h) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            uint4 r = make_uint4(0, 0, 0, 0), x = r;
+            if (mine) {
+                r = staged[stage][0][threadIdx.x];
+                if (NORM && rotate) x = staged[stage][NORM ? 1 : 0][threadIdx.x];
             }
+            if (rotate) {
+                P2 ya[NQ], yb[NQ], ga[NQ], gb[NQ];
+                V::unpack(r, ya, yb);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (h + u >= p.per_chunk) break;
-                if (t.rotate) {
-                    float ya[NP], yb[NP], ga[NP], gb[NP];
-                    V::unpack(r[u], ya, yb);
-#pragma unroll
-                    for (int i = 0; i < NP; ++i) {
-                        ga[i] = ya[i] * c[i] + yb[i] * s[i];
-                        gb[i] = yb[i] * c[i] - ya[i] * s[i];
-                    }
-                    if (NORM) {
-                        float xa[NP], xb[NP], ss = 0.f, gx = 0.f;
-                        V::unpack(x[u], xa, xb);
-#pragma unroll
-                        for (int i = 0; i < NP; ++i) {
-                            ss += xa[i] * xa[i] + xb[i] * xb[i];
-                            gx += ga[i] * wa[i] * xa[i] + gb[i] * wb[i] * xb[i];
-                        }
-                        const float q = rsqrtf(lanes_sum(ss, p.log_lanes) * p.inv_d + p.eps);
-                        const float m = lanes_sum(gx, p.log_lanes) * q * p.inv_d;
-#pragma unroll
-                        for (int i = 0; i < NP; ++i) {
-                            const float ha = xa[i] * q, hb = xb[i] * q;
-                            da[i] += ga[i] * ha;
-                            db[i] += gb[i] * hb;
-                            ga[i] = q * (ga[i] * wa[i] - ha * m);
-                            gb[i] = q * (gb[i] * wb[i] - hb * m);
-                        }
-                    }
-                    r[u] = V::pack(ga, gb);
+                for (int i = 0; i < NQ; ++i) {
+                    ga[i] = fma2(ya[i], c[i], mul2(yb[i], s[i]));
+                    gb[i] = fma2(yb[i], c[i], neg2(mul2(ya[i], s[i])));
                 }
-                if (mine && h0 + h + u < h1) at.store(dst + (h + u) * row, r[u]);
+                if (NORM) {
+                    P2 xa[NQ], xb[NQ], ss = 0, gx = 0;
+                    V::unpack(x, xa, xb);
+#pragma unroll
+                    for (int i = 0; i < NQ; ++i) {
+                        ss = fma2(xb[i], xb[i], fma2(xa[i], xa[i], ss));
+                        gx = fma2(mul2(gb[i], wb[i]), xb[i], fma2(mul2(ga[i], wa[i]), xa[i], gx));
+                    }
+                    const float2 f = both(ss), g = both(gx);
+                    float sum[2] = {f.x + f.y, g.x + g.y};      // of x^2 and of g w x
+                    lanes_sum<LOG, 2>(sum, log_lanes);
+                    const float q = rsqrtf(fmaf(sum[0], p.inv_d, p.eps)), m = sum[1] * q * p.inv_d;
+                    const P2 q2 = twice(q), less = twice(-m);
+#pragma unroll
+                    for (int i = 0; i < NQ; ++i) {
+                        const P2 ha = mul2(xa[i], q2), hb = mul2(xb[i], q2);
+                        da[i] = fma2(ga[i], ha, da[i]);
+                        db[i] = fma2(gb[i], hb, db[i]);
+                        ga[i] = mul2(q2, fma2(ha, less, mul2(ga[i], wa[i])));
+                        gb[i] = mul2(q2, fma2(hb, less, mul2(gb[i], wb[i])));
+                    }
+                }
+                r = V::pack(ga, gb);
             }
+            if (mine) at.store(dst, r);
+            dst += row;
+            fetch(stage);
+            stage = stage + 1 == kStages ? 0 : stage + 1;
         }
     }
-    if (NORM && p.want_dw && t.rotate) {      // (uniform over the block)
+    if (NORM && p.want_dw && rotate) {      // (uniform over the block)
         // group after group: sums[group][channel]
         constexpr int CH = V::CH;
-        float* mine = sums + (size_t)group * CH * (1 << p.log_lanes);
+        float* mine = sums + (size_t)group * CH * (1 << log_lanes);
         if (at.in) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int ca = HALF ? at.off_a / (int)sizeof(T) + i : l * CH + 2 * i, cb = HALF ? at.off_b / (int)sizeof(T) + i : ca + 1;
-                mine[ca] = da[i];
-                mine[cb] = db[i];
+                const float2 fa = both(da[i / 2]), fb = both(db[i / 2]);
+                mine[ca] = i & 1 ? fa.y : fa.x;
+                mine[cb] = i & 1 ? fb.y : fb.x;
             }
         }
         __syncthreads();
         float* part = p.part + ((size_t)(ti * p.chunks + chunk) * gridDim.x + blockIdx.x) * p.d;
         for (int ch = threadIdx.x; ch < p.d; ch += kThreads) {
             float v = 0.f;
-            for (int g = 0; g < groups; ++g) v += sums[(size_t)g * CH * (1 << p.log_lanes) + ch];
+            for (int g = 0; g < groups; ++g) v += sums[(size_t)g * CH * (1 << log_lanes) + ch];
             part[ch] = v;
         }
     }
@@ -330,8 +428,10 @@ __global__ void __launch_bounds__(kDwThreads) dw_kernel(const float* part, int r
     wait_for_previous_kernel();
     const float* mine = part + (size_t)blockIdx.y * rows * d;
     double v = 0.0;
-    if (ch < d)
+    if (ch < d) {
+#pragma unroll 8
         for (int r = slice; r < rows; r += 32) v += mine[(size_t)r * d + ch];
+    }
     sums[slice][threadIdx.x & 31] = v;
     __syncthreads();
     if (slice == 0 && ch < d) {
@@ -419,14 +519,23 @@ heads::Args common_args(const hla_heads* c, const int32_t* positions, int64_t po
 
 using Kernel = void (*)(heads::Args);
 
-template <template <typename, bool, bool> class K>
-Kernel pick(bool bf16, bool half, bool norm) {
-    if (bf16) return half ? (norm ? K<__nv_bfloat16, true, true>::get() : K<__nv_bfloat16, true, false>::get())
-                          : (norm ? K<__nv_bfloat16, false, true>::get() : K<__nv_bfloat16, false, false>::get());
-    return half ? (norm ? K<float, true, true>::get() : K<float, true, false>::get()) : (norm ? K<float, false, true>::get() : K<float, false, false>::get());
+template <template <typename, bool, bool, int> class K, typename T, int LOG>
+Kernel pick_of(bool half, bool norm) {
+    return half ? (norm ? K<T, true, true, LOG>::get() : K<T, true, false, LOG>::get()) : (norm ? K<T, false, true, LOG>::get() : K<T, false, false, LOG>::get());
 }
-template <typename T, bool HALF, bool NORM> struct Fwd { static Kernel get() { return heads::forward_kernel<T, HALF, NORM>; } };
-template <typename T, bool HALF, bool NORM> struct Bwd { static Kernel get() { return heads::backward_kernel<T, HALF, NORM>; } };
+// Rows of 128 and 64 channels have kernels that know their lanes.
+template <template <typename, bool, bool, int> class K>
+Kernel pick(const hla_heads* c) {
+    const bool half = c->cfg.pairing == HLA_PAIR_HALVES, norm = c->cfg.norm;
+    if (c->cfg.dtype == HLA_BF16) {
+        if (c->log_lanes == 4) return pick_of<K, __nv_bfloat16, 4>(half, norm);
+        return c->log_lanes == 3 ? pick_of<K, __nv_bfloat16, 3>(half, norm) : pick_of<K, __nv_bfloat16, 0>(half, norm);
+    }
+    if (c->log_lanes == 5) return pick_of<K, float, 5>(half, norm);
+    return c->log_lanes == 4 ? pick_of<K, float, 4>(half, norm) : pick_of<K, float, 0>(half, norm);
+}
+template <typename T, bool HALF, bool NORM, int LOG> struct Fwd { static Kernel get() { return heads::forward_kernel<T, HALF, NORM, LOG>; } };
+template <typename T, bool HALF, bool NORM, int LOG> struct Bwd { static Kernel get() { return heads::backward_kernel<T, HALF, NORM, LOG>; } };
 
 bool positions_ok(const hla_heads* c, const int32_t* positions, int64_t pos_batch) {
     if (!c->rot) return true;
@@ -536,7 +645,7 @@ hla_status hla_heads_forward(hla_heads* c, const hla_rows* q, const hla_rows* k,
     a.chunks = (a.H + a.per_chunk - 1) / a.per_chunk;
     const uint32_t units = (uint32_t)a.B * a.N * a.n_tensors * a.chunks;
     const int groups = heads::kThreads >> a.log_lanes;
-    const Kernel kern = pick<Fwd>(c->cfg.dtype == HLA_BF16, c->cfg.pairing == HLA_PAIR_HALVES, c->cfg.norm);
+    const Kernel kern = pick<Fwd>(c);
     kern<<<(units + groups - 1) / groups, heads::kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
     return cudaGetLastError() == cudaSuccess ? HLA_OK : HLA_ERR_CUDA;
 }
@@ -594,7 +703,7 @@ hla_status hla_heads_backward(hla_heads* c, const void* dQ, const void* dK, cons
     a.per_chunk = heads_per_run(c, a.n_tensors);
     a.chunks = (a.H + a.per_chunk - 1) / a.per_chunk;
     const int blocks = backward_blocks(c, a.n_tensors * a.chunks);
-    const Kernel kern = pick<Bwd>(c->cfg.dtype == HLA_BF16, c->cfg.pairing == HLA_PAIR_HALVES, c->cfg.norm);
+    const Kernel kern = pick<Bwd>(c);
     kern<<<dim3(blocks, a.n_tensors * a.chunks), heads::kThreads, 0, st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return HLA_ERR_CUDA;
     if (a.want_dw && !launch_behind(heads::dw_kernel, dim3((a.d + 31) / 32, normed), heads::kDwThreads, st, (const float*)a.part, a.chunks * blocks, a.d, sums[0], sums[1]))

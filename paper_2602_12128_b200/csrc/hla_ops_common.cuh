@@ -23,6 +23,7 @@ __device__ __forceinline__ float2 both(P2 v) { float2 r; asm("mov.b64 {%0, %1}, 
 __device__ __forceinline__ P2 fma2(P2 a, P2 b, P2 c) { P2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ P2 mul2(P2 a, P2 b) { P2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ P2 add2(P2 a, P2 b) { P2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ P2 neg2(P2 a) { return a ^ 0x8000000080000000ull; }
 __device__ __forceinline__ P2 twice(float x) { return pair(x, x); }
 
 // For a kernel launched with launch_behind: returns when the kernel before it in the stream has ended and its writes are visible.
