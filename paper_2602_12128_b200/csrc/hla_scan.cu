@@ -22,7 +22,7 @@
 namespace hla {
 namespace scan {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;                    // and a warp that exchanges states
 constexpr int kLanes = 16;                       // threads side by side on channels, two each
 constexpr int kRuns = kThreads / kLanes;
 template <typename T> constexpr int kRunOf = sizeof(T) == 2 ? 8 : 4;            // tokens of a thread: as many as its registers hold
@@ -139,12 +139,19 @@ struct Input {
     __device__ __forceinline__ Input(const char* base, long long token0, long long step_, int lane32) : at(base + token0 * step_ + (lane32 / S::kPerRow) * step_ + (lane32 % S::kPerRow) * 16), step(step_) {}
     // Copies the tokens first + (0 .. 2 kRun - 1) of the warp; tokens at `end` or behind are zeros, channels behind the last too.
     __device__ __forceinline__ void fetch(uint32_t to, int first, int end, int channels, int lane32, int stride) {
-        const int row = lane32 / S::kPerRow, col = lane32 % S::kPerRow, left = channels - col * (16 / (int)sizeof(T));
+        const int row = lane32 / S::kPerRow, col = lane32 % S::kPerRow;
+        static_assert(S::kHalf == S::kRun, "the second piece of a lane belongs to the second run");
+        to += row * S::kRowBytes + col * 16;
+        if (VEC && first + 2 * S::kRun <= end && channels >= kTile) {
+            copy16<T, true>(to, at, 16);
+            copy16<T, true>(to + S::kRunBytes, at + S::kHalf * step, 16);
+        } else {
+            const int left = channels - col * (16 / (int)sizeof(T));
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = row + i * S::kHalf;
-            const bool in = first + r < end;
-            copy16<T, VEC>(to + (r / S::kRun) * S::kRunBytes + (r % S::kRun) * S::kRowBytes + col * 16, in && left > 0 ? at + i * S::kHalf * step : at, in ? left : 0);
+            for (int i = 0; i < 2; ++i) {
+                const bool in = first + row + i * S::kHalf < end;
+                copy16<T, VEC>(to + i * S::kRunBytes, in && left > 0 ? at + i * S::kHalf * step : at, in ? left : 0);
+            }
         }
         at += stride * step;
     }
@@ -154,12 +161,6 @@ struct Input {
 __device__ __forceinline__ P2 load_state(const float* p, size_t i, bool live, bool second) {
     return p && live ? pair(p[i], second ? p[i + 1] : 0.f) : 0;
 }
-__device__ __forceinline__ void store_state(float* p, size_t i, bool second, P2 v) {
-    const float2 f = both(v);
-    p[i] = f.x;
-    if (second) p[i + 1] = f.y;
-}
-
 // a and 1 - a.  Where the memory is long a is near 1, and an error of a relative 2^-22 of every a would add up over it; so the smaller of
 // the two is formed first, with an error of its own size, and the larger is its difference to 1, correctly rounded.
 template <int GATE>
@@ -192,92 +193,114 @@ __device__ __forceinline__ void gate(P2 g, P2& a, P2& rest) {
 }
 
 struct Exchange {
-    ulonglong2 warps[kRuns / 2][kLanes];                 // maps (A, H) of this block's warps, two runs each
-    ulonglong2 blocks[2][kMaxCluster][kLanes];           // of the cluster's blocks, of this piece and the next
-    uint64_t full[2];                                    // barriers: the maps of all blocks are there
+    float2 warps_a[kRuns / 2][kLanes], warps_h[kRuns / 2][kLanes];      // maps (A, H) of this block's warps, two runs each
+    float2 before[kRuns / 2][kLanes];                                   // the state before each warp's tokens
+    float2 blocks[2][kMaxCluster][kTile];                               // maps of the cluster's blocks, of this piece and the next
+    uint64_t full[2];                                                   // barriers: the maps of all blocks are there
 };
 
+__device__ __forceinline__ void arrive_at(int barrier) { asm volatile("bar.arrive %0, %1;" ::"r"(barrier), "n"(kThreads + 32) : "memory"); }
+__device__ __forceinline__ void wait_at(int barrier) { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kThreads + 32) : "memory"); }
+constexpr int kMapsThere = 1, kStatesThere = 2;
+
+// The last warp of a block: a channel per lane.  It composes the maps of the block's warps, hands the result to the blocks of the cluster and,
+// from theirs, finds the state before each warp's tokens.  (Done by every thread for itself, this was five instructions of 34 an element.)
+//
 // Every map of a piece is written by its block straight into the shared memory of all blocks of the cluster and counted by their barriers.
 // A buffer is written again two pieces later: by then its writer has had this block's map of the piece between, which this block sends
 // behind its reads of the buffer.
-struct Cluster {
-    Exchange& e;
-    int lane, run, rank, blocks;
-    bool lost;
-
-    __device__ __forceinline__ Cluster(Exchange& x) : e(x), lane(threadIdx.x % kLanes), run(threadIdx.x / kLanes), rank(cluster_rank()), blocks(cluster_blocks()), lost(false) {}
-    __device__ __forceinline__ void start() {
-        if (threadIdx.x == 0) {
-            tc::mbar_init(&e.full[0], 1);
-            tc::mbar_init(&e.full[1], 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
-        cluster_sync();
-    }
-    // From the map (A, H) of this thread's run: the state before its first token; `carry`, the state before the cluster's piece, becomes
-    // the one behind it.  Every thread of the cluster calls this once a piece.
-    __device__ __forceinline__ P2 state_before(P2 A, P2 H, P2& carry, int piece) {
-        const int buffer = piece & 1, warp = run >> 1;
-        const bool second = run & 1;
-        // the other run of the warp; the second run's thread forms the map of both
-        const P2 qa = __shfl_xor_sync(0xffffffffu, A, kLanes), qh = __shfl_xor_sync(0xffffffffu, H, kLanes);
-        const P2 WA = mul2(A, qa), WH = fma2(A, qh, H);
-        if (threadIdx.x == 0) tc::mbar_arrive_expect_tx(&e.full[buffer], blocks * kLanes * (int)sizeof(ulonglong2));
-        if (second) e.warps[warp][lane] = make_ulonglong2(WA, WH);
-        __syncthreads();
-        P2 PA = twice(1.f), PH = 0;
+__device__ __forceinline__ float exchange(Exchange& e, int pieces, int rank, int blocks, float carry) {
+    const int lane = threadIdx.x & 31;
+    const float *wa = &e.warps_a[0][0].x + lane, *wh = &e.warps_h[0][0].x + lane;
+    float* before = &e.before[0][0].x + lane;
+    bool lost = false;
+    for (int s = 0; s < pieces; ++s) {
+        const int buffer = s & 1;
+        if (lane == 0) tc::mbar_arrive_expect_tx(&e.full[buffer], blocks * kTile * (int)sizeof(float2));
+        wait_at(kMapsThere);
+        float PA[kRuns / 2], PH[kRuns / 2], A = 1.f, H = 0.f;
 #pragma unroll
-        for (int w = 0; w < kRuns / 2 - 1; ++w) {
-            if (w >= warp) break;
-            const ulonglong2 q = e.warps[w][lane];
-            PH = fma2(q.x, PH, q.y);
-            PA = mul2(q.x, PA);
+        for (int w = 0; w < kRuns / 2; ++w) {
+            PA[w] = A;
+            PH[w] = H;
+            const float a = wa[w * kTile], h = wh[w * kTile];
+            H = fmaf(a, H, h);
+            A *= a;
         }
-        if (run == kRuns - 1) {
-            const float2 ta = both(mul2(WA, PA)), th = both(fma2(WA, PH, WH));
-            const uint32_t to = tc::smem_u32(&e.blocks[buffer][rank][lane]), bar = tc::smem_u32(&e.full[buffer]);
-            for (int i = 0; i < blocks; ++i)
-                asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(of_block(to, i)), "f"(ta.x), "f"(ta.y), "f"(th.x),
-                             "f"(th.y), "r"(of_block(bar, i))
-                             : "memory");
-        }
-        if (second) {
-            PH = fma2(qa, PH, qh);
-            PA = mul2(qa, PA);
-        }
-        if (!lost && !tc::mbar_wait(&e.full[buffer], (piece >> 1) & 1)) {      // (two seconds: the outputs from here on are not numbers)
+        const uint32_t to = tc::smem_u32(&e.blocks[buffer][rank][lane]), bar = tc::smem_u32(&e.full[buffer]);
+        for (int i = 0; i < blocks; ++i)
+            asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(of_block(to, i)), "f"(A), "f"(H), "r"(of_block(bar, i)) : "memory");
+        if (!lost && !tc::mbar_wait(&e.full[buffer], (s >> 1) & 1)) {      // (two seconds: the outputs from here on are not numbers)
             lost = true;
-            carry = twice(__int_as_float(0x7fc00000));
+            carry = __int_as_float(0x7fc00000);
         }
-        P2 mine = carry;
-        for (int i = 0; i < blocks; ++i) {
+        float mine = carry;
+#pragma unroll
+        for (int i = 0; i < kMaxCluster; ++i) {
+            if (i >= blocks) break;
             if (i == rank) mine = carry;
-            const ulonglong2 q = e.blocks[buffer][i][lane];
-            carry = fma2(q.x, carry, q.y);
+            const float2 q = e.blocks[buffer][i][lane];
+            carry = fmaf(q.x, carry, q.y);
         }
-        return fma2(PA, mine, PH);
+#pragma unroll
+        for (int w = 0; w < kRuns / 2; ++w) before[w * kTile] = fmaf(PA[w], mine, PH[w]);
+        arrive_at(kStatesThere);
     }
-};
+    return carry;
+}
+
+// A warp's part of it: from the map (A, H) of this thread's run the state before its first token.  `during` runs while the maps are under way.
+template <typename F>
+__device__ __forceinline__ P2 state_before(Exchange& e, P2 A, P2 H, int warp, int lane, bool second, F during) {
+    // the other run of the warp: (qa, qh); the second run's thread forms the map of both
+    const P2 qa = __shfl_xor_sync(0xffffffffu, A, kLanes), qh = __shfl_xor_sync(0xffffffffu, H, kLanes);
+    if (second) {
+        e.warps_a[warp][lane] = both(mul2(A, qa));
+        e.warps_h[warp][lane] = both(fma2(A, qh, H));
+    }
+    arrive_at(kMapsThere);
+    during();
+    wait_at(kStatesThere);
+    const float2 f = e.before[warp][lane];
+    const P2 h = pair(f.x, f.y);
+    return second ? fma2(qa, h, qh) : h;
+}
+
+__device__ __forceinline__ void start(Exchange& e) {
+    if (threadIdx.x == 0) {
+        tc::mbar_init(&e.full[0], 1);
+        tc::mbar_init(&e.full[1], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cluster_sync();
+}
+
+// One block of the cluster: the exchanging warp, its state going in and out.
+__device__ __forceinline__ void exchange_warp(Exchange& e, const Args& p, int rank, int blocks, int b) {
+    const int c = blockIdx.y * kTile + (threadIdx.x & 31);
+    const size_t at = (size_t)b * p.C + c;
+    const float carry = exchange(e, p.pieces, rank, blocks, p.in && c < p.C ? p.in[at] : 0.f);
+    if (p.last && rank == 0 && c < p.C) p.last[at] = carry;
+}
 
 template <typename T, int GATE, bool CONVEX, bool VEC>
-__global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_constant__ Args p) {
+__global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_constant__ Args p) {
     using V = Two<T>;
     using S = Stage<T>;
     constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>, kInputs = 2, kStages = 3;
     __shared__ Exchange e;
     extern __shared__ __align__(128) char staged[];
-    Cluster cl(e);
-    const int lane32 = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.y * kTile + 2 * cl.lane, b = blockIdx.z;
+    const int lane32 = threadIdx.x & 31, lane = lane32 % kLanes, warp = threadIdx.x >> 5, rank = cluster_rank(), blocks = cluster_blocks();
+    const bool late = lane32 >= kLanes;      // the second run of the warp
+    const int c = blockIdx.y * kTile + 2 * lane, b = blockIdx.z;
     const int channels = p.C - (int)blockIdx.y * kTile;
     const bool live = c < p.C, second = c + 1 < p.C;
-    const size_t at_state = (size_t)b * p.C + c;
-    P2 carry = load_state(p.in, at_state, live, second);
     const long long gs = p.g_token * (int)sizeof(T), xs = p.x_token * (int)sizeof(T), os = (long long)p.C * (int)sizeof(T);
-    const int stride = cl.blocks * kPiece, tile = (int)blockIdx.y * kTile;
-    int w0 = cl.rank * kPiece + warp * 2 * kRun, t0 = w0 + (cl.run & 1) * kRun;      // first token of the warp, of the thread
+    const int stride = blocks * kPiece, tile = (int)blockIdx.y * kTile;
+    int w0 = rank * kPiece + warp * 2 * kRun, t0 = w0 + late * kRun;      // first token of the warp, of the thread
     Input<T, VEC> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T), w0, gs, lane32), x(p.x + (b * p.x_batch + tile) * (int)sizeof(T), w0, xs, lane32);
     char* po = p.out0 + ((long long)b * p.N * p.C + c) * (int)sizeof(T) + t0 * os;
-    const uint32_t mine = tc::smem_u32(staged) + warp * (kStages * kInputs * S::kBytes), own = (cl.run & 1) * S::kRunBytes + cl.lane * 2 * (int)sizeof(T);
+    const uint32_t mine = tc::smem_u32(staged) + warp * (kStages * kInputs * S::kBytes), own = late * S::kRunBytes + lane * 2 * (int)sizeof(T);
     auto fetch = [&](int piece, int stage) {
         if (piece < p.pieces) {
             const uint32_t to = mine + stage * (kInputs * S::kBytes);
@@ -286,9 +309,16 @@ __global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_const
         }
         commit();
     };
+    if (warp < kThreads / 32) {
 #pragma unroll
-    for (int i = 0; i < kStages; ++i) fetch(i, i);
-    cl.start();
+        for (int i = 0; i < kStages; ++i) fetch(i, i);
+    }
+    start(e);
+    if (warp == kThreads / 32) {
+        exchange_warp(e, p, rank, blocks, b);
+        cluster_sync();      // no block leaves while another may still write into its shared memory
+        return;
+    }
     for (int s = 0, stage = 0; s < p.pieces; ++s) {
         arrived<kStages - 1>();
         const uint32_t from = mine + stage * (kInputs * S::kBytes) + own;
@@ -300,9 +330,6 @@ __global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_const
             u[k] = V::get(read<typename V::Raw>(from + S::kBytes + k * S::kRowBytes));
             if (CONVEX) u[k] = mul2(rest, u[k]);
         }
-        __syncwarp();
-        fetch(s + kStages, stage);
-        stage = stage + 1 == kStages ? 0 : stage + 1;
         const bool whole = live && t0 + kRun <= p.N;
         if (!whole) {      // behind the end nothing changes
 #pragma unroll
@@ -315,7 +342,11 @@ __global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_const
             H = fma2(a[k], H, u[k]);
             A = mul2(a[k], A);
         }
-        P2 h = cl.state_before(A, H, carry, s);
+        P2 h = state_before(e, A, H, warp, lane, late, [&] {
+            __syncwarp();
+            fetch(s + kStages, stage);
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+        });
         if (whole) {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
@@ -332,35 +363,33 @@ __global__ void __launch_bounds__(kThreads, 3) forward_kernel(const __grid_const
         po += stride * os;
         t0 += stride;
     }
-    if (p.last && cl.rank == 0 && cl.run == 0 && live) store_state(p.last, at_state, second, carry);
-    cluster_sync();      // no block leaves while another may still write into its shared memory
+    cluster_sync();
 }
 
 // Tokens are counted from the end: i = N - 1 - t; pointers go down.
 template <typename T, int GATE, bool CONVEX, bool VEC>
-__global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_constant__ Args p) {
+__global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid_constant__ Args p) {
     using V = Two<T>;
     using Raw = typename V::Raw;
     using S = Stage<T>;
     constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>, kInputs = CONVEX ? 4 : 3, kStages = 2;
     __shared__ Exchange e;
     extern __shared__ __align__(128) char staged[];
-    Cluster cl(e);
-    const int lane32 = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.y * kTile + 2 * cl.lane, b = blockIdx.z;
+    const int lane32 = threadIdx.x & 31, lane = lane32 % kLanes, warp = threadIdx.x >> 5, rank = cluster_rank(), blocks = cluster_blocks();
+    const bool late = lane32 >= kLanes;      // the second run of the warp
+    const int c = blockIdx.y * kTile + 2 * lane, b = blockIdx.z;
     const int channels = p.C - (int)blockIdx.y * kTile;
     const bool live = c < p.C, second = c + 1 < p.C;
-    const size_t at_state = (size_t)b * p.C + c;
-    P2 carry = load_state(p.in, at_state, live, second);
-    const P2 h0 = load_state(p.h0, at_state, live, second);
+    const P2 h0 = load_state(p.h0, (size_t)b * p.C + c, live, second);
     const long long gs = p.g_token * (int)sizeof(T), xs = p.x_token * (int)sizeof(T), os = (long long)p.C * (int)sizeof(T);
-    const int stride = cl.blocks * kPiece, tile = (int)blockIdx.y * kTile;
-    int w0 = cl.rank * kPiece + warp * 2 * kRun, i0 = w0 + (cl.run & 1) * kRun;
+    const int stride = blocks * kPiece, tile = (int)blockIdx.y * kTile;
+    int w0 = rank * kPiece + warp * 2 * kRun, i0 = w0 + late * kRun;
     const long long dense = ((long long)b * p.N * p.C + tile) * (int)sizeof(T), end = p.N - 1;
     Input<T, VEC> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T) + end * gs, w0, -gs, lane32), d(p.dh + dense + end * os, w0, -os, lane32),
         h(p.h + dense + (end - 1) * os, w0, -os, lane32), x(CONVEX ? p.x + (b * p.x_batch + tile) * (int)sizeof(T) + end * xs : nullptr, w0, -xs, lane32);
-    const long long out = dense + 2 * cl.lane * (int)sizeof(T) + (end - i0) * os;
+    const long long out = dense + 2 * lane * (int)sizeof(T) + (end - i0) * os;
     char *po0 = p.out0 + out, *po1 = p.out1 + out;
-    const uint32_t mine = tc::smem_u32(staged) + warp * (kStages * kInputs * S::kBytes), own = (cl.run & 1) * S::kRunBytes + cl.lane * 2 * (int)sizeof(T);
+    const uint32_t mine = tc::smem_u32(staged) + warp * (kStages * kInputs * S::kBytes), own = late * S::kRunBytes + lane * 2 * (int)sizeof(T);
     auto fetch = [&](int piece, int stage) {
         if (piece < p.pieces) {
             const uint32_t to = mine + stage * (kInputs * S::kBytes);
@@ -372,9 +401,16 @@ __global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_cons
         }
         commit();
     };
+    if (warp < kThreads / 32) {
 #pragma unroll
-    for (int i = 0; i < kStages; ++i) fetch(i, i);
-    cl.start();
+        for (int i = 0; i < kStages; ++i) fetch(i, i);
+    }
+    start(e);
+    if (warp == kThreads / 32) {
+        exchange_warp(e, p, rank, blocks, b);
+        cluster_sync();      // no block leaves while another may still write into its shared memory
+        return;
+    }
     for (int s = 0, stage = 0; s < p.pieces; ++s) {
         arrived<kStages - 1>();
         const uint32_t from = mine + stage * (kInputs * S::kBytes) + own;
@@ -388,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_cons
             M = mul2(a[k], k ? add2(dk, M) : dk);
             A = k ? mul2(a[k], A) : a[k];
         }
-        P2 mu = cl.state_before(A, M, carry, s);
+        P2 mu = state_before(e, A, M, warp, lane, late, [] {});
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
             const P2 lam = add2(V::get(read<Raw>(from + S::kBytes + k * S::kRowBytes)), mu);
@@ -411,7 +447,6 @@ __global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_cons
         po1 -= stride * os;
         i0 += stride;
     }
-    if (p.last && cl.rank == 0 && cl.run == 0 && live) store_state(p.last, at_state, second, carry);
     cluster_sync();
 }
 
@@ -470,11 +505,14 @@ bool vectors(const hla_scan* c, const scan::Args& a) {
 hla_status launch(const hla_scan* c, Kernel kern, int bytes, scan::Args& a, cudaStream_t st) {
     int blocks = 1;      // of a cluster
     const int piece = c->cfg.dtype == HLA_BF16 ? scan::kPieceOf<__nv_bfloat16> : scan::kPieceOf<float>;
-    while (blocks < scan::kMaxCluster && blocks * piece < a.N) blocks *= 2;
+    // as many as sequences and channels leave room for (three blocks an SM): a second wave would wait for the first, and with fewer blocks in a
+    // cluster an exchange is shorter.  Backward of 2 x 32760 tokens, 1536 channels: 8 blocks a cluster (1.7 waves) 247 us, 4 blocks 2XX us
+    const long long columns = (long long)((a.C + scan::kTile - 1) / scan::kTile) * c->cfg.B;
+    while (blocks < scan::kMaxCluster && blocks * piece < a.N && 2 * blocks * columns <= 3ll * c->sm_count) blocks *= 2;
     a.pieces = (int)((a.N + (long long)blocks * piece - 1) / (blocks * piece));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks, (a.C + scan::kTile - 1) / scan::kTile, c->cfg.B);
-    cfg.blockDim = dim3(scan::kThreads);
+    cfg.blockDim = dim3(scan::kThreads + 32);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return HLA_ERR_CUDA;
