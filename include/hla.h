@@ -454,9 +454,12 @@ typedef struct {
     int64_t g_batch_stride, g_token_stride;
 } hla_scan_config;
 hla_status hla_scan_create(const hla_scan_config *cfg, hla_scan **out);
-hla_status hla_scan_forward(hla_scan *ctx, const void *x, const void *g, const void *h0, void *h, void *h_last, void *cuda_stream);
+/* Scratch of both calls (0 where there are channels enough to fill the machine: a long sequence of few channels runs in parts). */
+size_t hla_scan_workspace_bytes(const hla_scan *ctx);
+hla_status hla_scan_forward(hla_scan *ctx, const void *x, const void *g, const void *h0, void *h, void *h_last, void *workspace, size_t workspace_bytes,
+                            void *cuda_stream);
 hla_status hla_scan_backward(hla_scan *ctx, const void *x, const void *g, const void *h0, const void *h, const void *dh, const void *dh_last,
-                             void *dx, void *dg, void *dh0, void *cuda_stream);
+                             void *dx, void *dg, void *dh0, void *workspace, size_t workspace_bytes, void *cuda_stream);
 hla_status hla_scan_destroy(hla_scan *ctx);
 
 const char *hla_status_string(hla_status s);

@@ -22,7 +22,7 @@ EXPORTS = [
     "hla_destroy", "hla_status_string",
     "hla_heads_create", "hla_heads_workspace_bytes", "hla_heads_forward", "hla_heads_backward", "hla_heads_destroy",
     "hla_adamw_create", "hla_adamw_set_grads", "hla_adamw_workspace_bytes", "hla_adamw_step", "hla_adamw_destroy",
-    "hla_scan_create", "hla_scan_forward", "hla_scan_backward", "hla_scan_destroy",
+    "hla_scan_create", "hla_scan_workspace_bytes", "hla_scan_forward", "hla_scan_backward", "hla_scan_destroy",
 ]
 
 
@@ -160,13 +160,13 @@ def load_library(rebuild: bool = False) -> ctypes.CDLL:
         "hla_adamw_step": [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p],
         "hla_adamw_destroy": [c_void_p],
         "hla_scan_create": [POINTER(HlaScanConfig), POINTER(c_void_p)],
-        "hla_scan_forward": [c_void_p] * 7,
-        "hla_scan_backward": [c_void_p] * 11,
+        "hla_scan_forward": [c_void_p] * 7 + [c_size_t, c_void_p],
+        "hla_scan_backward": [c_void_p] * 11 + [c_size_t, c_void_p],
         "hla_scan_destroy": [c_void_p],
     }.items():
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = c_int32
-    for name in ("hla_heads_workspace_bytes", "hla_adamw_workspace_bytes"):
+    for name in ("hla_heads_workspace_bytes", "hla_adamw_workspace_bytes", "hla_scan_workspace_bytes"):
         getattr(lib, name).argtypes = [c_void_p]
         getattr(lib, name).restype = c_size_t
     lib.hla_status_string.argtypes = [c_int32]
@@ -741,6 +741,9 @@ class Scan(_Owner):
         self.device = device
         self._shape, self._state = torch.Size((B, N, C)), torch.Size((B, C))
         self._new, self._new_state = _Maker(self._shape, self.torch_dtype, device), _Maker(self._state, torch.float32, device)
+        self._need = int(load_library().hla_scan_workspace_bytes(self.ctx))
+        self.workspace = torch.empty(self._need, dtype=torch.uint8, device=device) if device and self._need else None
+        self._scratch = _ptr(self.workspace)
         self._forward, self._backward = load_library().hla_scan_forward, load_library().hla_scan_backward
 
     def _make(self):
@@ -778,7 +781,7 @@ class Scan(_Owner):
         h = self._new(dev) if h is None else h
         h_last = self._new_state(dev) if h_last is None else h_last
         st = self._forward(self.ctx, x.data_ptr(), g.data_ptr(), _dense(h0, "h0", f32, self._state, dev), _dense(h, "h", self.torch_dtype, self._shape, dev),
-                           _dense(h_last, "h_last", f32, self._state, dev), _stream(stream))
+                           _dense(h_last, "h_last", f32, self._state, dev), self._scratch, self._need, _stream(stream))
         if st != HLA_OK:
             raise HlaError(st, "hla_scan_forward")
         return h, h_last
@@ -792,7 +795,7 @@ class Scan(_Owner):
         dh0 = self._new_state(dev) if h0 is not None else None
         st = self._backward(self.ctx, x.data_ptr(), g.data_ptr(), _dense(h0, "h0", f32, self._state, dev), _dense(h, "h", dt, shape, dev),
                             _dense(dh, "dh", dt, shape, dev), _dense(dlast, "dlast", f32, self._state, dev), _dense(dx, "dx", dt, shape, dev),
-                            _dense(dg, "dg", dt, shape, dev), 0 if dh0 is None else dh0.data_ptr(), _stream(stream))
+                            _dense(dg, "dg", dt, shape, dev), 0 if dh0 is None else dh0.data_ptr(), self._scratch, self._need, _stream(stream))
         if st != HLA_OK:
             raise HlaError(st, "hla_scan_backward")
         return dx, dg, dh0

@@ -40,6 +40,8 @@ struct Args {
     const float *in;                             // state that comes in (forward h0, backward dlast), or null
     const float *h0;                             // backward: the state before the first token, or null
     float* last;                                 // state that goes out (forward h_N, backward dh0), or null
+    int segments, summary;                       // parts of a sequence that run side by side; 1: only their maps are wanted
+    float2* maps;                                // [segment][B][C] maps of the segments, and the state that comes in
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
@@ -209,10 +211,11 @@ constexpr int kMapsThere = 1, kStatesThere = 2;
 // Every map of a piece is written by its block straight into the shared memory of all blocks of the cluster and counted by their barriers.
 // A buffer is written again two pieces later: by then its writer has had this block's map of the piece between, which this block sends
 // behind its reads of the buffer.
-__device__ __forceinline__ float exchange(Exchange& e, int pieces, int rank, int blocks, float carry) {
+__device__ __forceinline__ float2 exchange(Exchange& e, int pieces, int rank, int blocks, float carry) {
     const int lane = threadIdx.x & 31;
     const float *wa = &e.warps_a[0][0].x + lane, *wh = &e.warps_h[0][0].x + lane;
     float* before = &e.before[0][0].x + lane;
+    float product = 1.f;      // of all factors: (product, carry) is the map of all pieces
     bool lost = false;
     for (int s = 0; s < pieces; ++s) {
         const int buffer = s & 1;
@@ -241,12 +244,13 @@ __device__ __forceinline__ float exchange(Exchange& e, int pieces, int rank, int
             if (i == rank) mine = carry;
             const float2 q = e.blocks[buffer][i][lane];
             carry = fmaf(q.x, carry, q.y);
+            product *= q.x;
         }
 #pragma unroll
         for (int w = 0; w < kRuns / 2; ++w) before[w * kTile] = fmaf(PA[w], mine, PH[w]);
         arrive_at(kStatesThere);
     }
-    return carry;
+    return make_float2(product, carry);
 }
 
 // A warp's part of it: from the map (A, H) of this thread's run the state before its first token.  `during` runs while the maps are under way.
@@ -275,12 +279,28 @@ __device__ __forceinline__ void start(Exchange& e) {
     cluster_sync();
 }
 
-// One block of the cluster: the exchanging warp, its state going in and out.
-__device__ __forceinline__ void exchange_warp(Exchange& e, const Args& p, int rank, int blocks, int b) {
+// The exchanging warp of a block: its state going in, through the maps of the segments before its own, and out.
+__device__ __forceinline__ void exchange_warp(Exchange& e, const Args& p, int rank, int blocks, int b, int segment) {
     const int c = blockIdx.y * kTile + (threadIdx.x & 31);
-    const size_t at = (size_t)b * p.C + c;
-    const float carry = exchange(e, p.pieces, rank, blocks, p.in && c < p.C ? p.in[at] : 0.f);
-    if (p.last && rank == 0 && c < p.C) p.last[at] = carry;
+    const bool live = c < p.C;
+    const size_t at = (size_t)b * p.C + c, all = (size_t)(gridDim.z / p.segments) * p.C;
+    float carry = 0.f;
+    if (!p.summary && live) {
+        // (the state that goes out may lie over the one that comes in: with segments, which end in any order, its copy from the first pass is read)
+        if (p.in) carry = p.segments > 1 ? p.maps[p.segments * all + at].x : p.in[at];
+        for (int i = 0; i < segment; ++i) {
+            const float2 m = p.maps[i * all + at];
+            carry = fmaf(m.x, carry, m.y);
+        }
+    }
+    const float2 map = exchange(e, p.pieces, rank, blocks, carry);
+    if (rank == 0 && live) {
+        if (p.summary) {
+            p.maps[segment * all + at] = map;
+            if (segment == 0 && p.in) p.maps[p.segments * all + at] = make_float2(p.in[at], 0.f);
+        }
+        else if (p.last && segment == p.segments - 1) p.last[at] = map.y;
+    }
 }
 
 template <typename T, int GATE, bool CONVEX, bool VEC>
@@ -292,12 +312,12 @@ __global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_
     extern __shared__ __align__(128) char staged[];
     const int lane32 = threadIdx.x & 31, lane = lane32 % kLanes, warp = threadIdx.x >> 5, rank = cluster_rank(), blocks = cluster_blocks();
     const bool late = lane32 >= kLanes;      // the second run of the warp
-    const int c = blockIdx.y * kTile + 2 * lane, b = blockIdx.z;
+    const int c = blockIdx.y * kTile + 2 * lane, b = blockIdx.z / p.segments, segment = blockIdx.z % p.segments;
     const int channels = p.C - (int)blockIdx.y * kTile;
     const bool live = c < p.C, second = c + 1 < p.C;
     const long long gs = p.g_token * (int)sizeof(T), xs = p.x_token * (int)sizeof(T), os = (long long)p.C * (int)sizeof(T);
     const int stride = blocks * kPiece, tile = (int)blockIdx.y * kTile;
-    int w0 = rank * kPiece + warp * 2 * kRun, t0 = w0 + late * kRun;      // first token of the warp, of the thread
+    int w0 = segment * p.pieces * stride + rank * kPiece + warp * 2 * kRun, t0 = w0 + late * kRun;      // first token of the warp, of the thread
     Input<T, VEC> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T), w0, gs, lane32), x(p.x + (b * p.x_batch + tile) * (int)sizeof(T), w0, xs, lane32);
     char* po = p.out0 + ((long long)b * p.N * p.C + c) * (int)sizeof(T) + t0 * os;
     const uint32_t mine = tc::smem_u32(staged) + warp * (kStages * kInputs * S::kBytes), own = late * S::kRunBytes + lane * 2 * (int)sizeof(T);
@@ -315,7 +335,7 @@ __global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_
     }
     start(e);
     if (warp == kThreads / 32) {
-        exchange_warp(e, p, rank, blocks, b);
+        exchange_warp(e, p, rank, blocks, b, segment);
         cluster_sync();      // no block leaves while another may still write into its shared memory
         return;
     }
@@ -347,7 +367,8 @@ __global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_
             fetch(s + kStages, stage);
             stage = stage + 1 == kStages ? 0 : stage + 1;
         });
-        if (whole) {
+        if (p.summary) {
+        } else if (whole) {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
                 h = fma2(a[k], h, u[k]);
@@ -377,13 +398,13 @@ __global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid
     extern __shared__ __align__(128) char staged[];
     const int lane32 = threadIdx.x & 31, lane = lane32 % kLanes, warp = threadIdx.x >> 5, rank = cluster_rank(), blocks = cluster_blocks();
     const bool late = lane32 >= kLanes;      // the second run of the warp
-    const int c = blockIdx.y * kTile + 2 * lane, b = blockIdx.z;
+    const int c = blockIdx.y * kTile + 2 * lane, b = blockIdx.z / p.segments, segment = blockIdx.z % p.segments;
     const int channels = p.C - (int)blockIdx.y * kTile;
     const bool live = c < p.C, second = c + 1 < p.C;
     const P2 h0 = load_state(p.h0, (size_t)b * p.C + c, live, second);
     const long long gs = p.g_token * (int)sizeof(T), xs = p.x_token * (int)sizeof(T), os = (long long)p.C * (int)sizeof(T);
     const int stride = blocks * kPiece, tile = (int)blockIdx.y * kTile;
-    int w0 = rank * kPiece + warp * 2 * kRun, i0 = w0 + late * kRun;
+    int w0 = segment * p.pieces * stride + rank * kPiece + warp * 2 * kRun, i0 = w0 + late * kRun;
     const long long dense = ((long long)b * p.N * p.C + tile) * (int)sizeof(T), end = p.N - 1;
     Input<T, VEC> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T) + end * gs, w0, -gs, lane32), d(p.dh + dense + end * os, w0, -os, lane32),
         h(p.h + dense + (end - 1) * os, w0, -os, lane32), x(CONVEX ? p.x + (b * p.x_batch + tile) * (int)sizeof(T) + end * xs : nullptr, w0, -xs, lane32);
@@ -396,8 +417,8 @@ __global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid
             const int first = w0 + piece * stride;
             g.fetch(to, first, p.N, channels, lane32, stride);
             d.fetch(to + S::kBytes, first, p.N, channels, lane32, stride);
-            h.fetch(to + 2 * S::kBytes, first, p.N - 1, channels, lane32, stride);      // (the state before token 0 is h0)
-            if (CONVEX) x.fetch(to + 3 * S::kBytes, first, p.N, channels, lane32, stride);
+            if (!p.summary) h.fetch(to + 2 * S::kBytes, first, p.N - 1, channels, lane32, stride);      // (the state before token 0 is h0)
+            if (CONVEX && !p.summary) x.fetch(to + 3 * S::kBytes, first, p.N, channels, lane32, stride);
         }
         commit();
     };
@@ -407,7 +428,7 @@ __global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid
     }
     start(e);
     if (warp == kThreads / 32) {
-        exchange_warp(e, p, rank, blocks, b);
+        exchange_warp(e, p, rank, blocks, b, segment);
         cluster_sync();      // no block leaves while another may still write into its shared memory
         return;
     }
@@ -427,6 +448,7 @@ __global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid
         P2 mu = state_before(e, A, M, warp, lane, late, [] {});
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
+            if (p.summary) break;
             const P2 lam = add2(V::get(read<Raw>(from + S::kBytes + k * S::kRowBytes)), mu);
             mu = mul2(a[k], lam);
             P2 w = V::get(read<Raw>(from + 2 * S::kBytes + k * S::kRowBytes));
@@ -502,16 +524,35 @@ bool vectors(const hla_scan* c, const scan::Args& a) {
     return !((a.C | a.x_batch | a.x_token | a.g_batch | a.g_token) * elt_size(c->cfg.dtype) & 15) && at % 16 == 0;
 }
 
-hla_status launch(const hla_scan* c, Kernel kern, int bytes, scan::Args& a, cudaStream_t st) {
+long long columns_of(const hla_scan* c) { return (long long)((c->cfg.C + scan::kTile - 1) / scan::kTile) * c->cfg.B; }
+
+// Parts of a sequence that run side by side: a first pass finds the map of each, and the pass proper starts every part from the states that the
+// maps before it give.  It reads the inputs twice, so it is taken where at least four parts fit on the machine next to one another and each
+// still has several exchanges (75600 tokens of 64 channels: XX us in one part, YY us in 13).
+int segments_of(const hla_scan* c, int blocks, long long pieces) {
+    long long n = 3ll * c->sm_count / (blocks * columns_of(c));
+    if (n > pieces / 2) n = pieces / 2;
+    return n < 4 ? 1 : (int)n;
+}
+
+hla_status launch(const hla_scan* c, Kernel kern, int bytes, scan::Args& a, void* workspace, size_t workspace_bytes, cudaStream_t st) {
     int blocks = 1;      // of a cluster
     const int piece = c->cfg.dtype == HLA_BF16 ? scan::kPieceOf<__nv_bfloat16> : scan::kPieceOf<float>;
     // as many as sequences and channels leave room for (three blocks an SM): a second wave would wait for the first, and with fewer blocks in a
-    // cluster an exchange is shorter.  Backward of 2 x 32760 tokens, 1536 channels: 8 blocks a cluster (1.7 waves) 247 us, 4 blocks 2XX us
-    const long long columns = (long long)((a.C + scan::kTile - 1) / scan::kTile) * c->cfg.B;
-    while (blocks < scan::kMaxCluster && blocks * piece < a.N && 2 * blocks * columns <= 3ll * c->sm_count) blocks *= 2;
-    a.pieces = (int)((a.N + (long long)blocks * piece - 1) / (blocks * piece));
+    // cluster an exchange is shorter.  Backward of 2 x 32760 tokens, 1536 channels: 8 blocks a cluster (1.7 waves) 247 us, 4 blocks 233 us
+    const long long columns = columns_of(c), room = 3ll * c->sm_count;
+    while (blocks < scan::kMaxCluster && blocks * piece < a.N && 2 * blocks * columns <= room) blocks *= 2;
+    const long long total = ((long long)a.N + blocks * piece - 1) / (blocks * piece);
+    a.segments = segments_of(c, blocks, total);
+    a.pieces = (int)((total + a.segments - 1) / a.segments);
+    a.segments = (int)((total + a.pieces - 1) / a.pieces);
+    a.maps = static_cast<float2*>(workspace);
+    if (a.segments > 1) {
+        if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
+        if (workspace_bytes < hla_scan_workspace_bytes(c)) return HLA_ERR_WORKSPACE;
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(blocks, (a.C + scan::kTile - 1) / scan::kTile, c->cfg.B);
+    cfg.gridDim = dim3(blocks, (a.C + scan::kTile - 1) / scan::kTile, c->cfg.B * a.segments);
     cfg.blockDim = dim3(scan::kThreads + 32);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
@@ -522,6 +563,11 @@ hla_status launch(const hla_scan* c, Kernel kern, int bytes, scan::Args& a, cuda
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
+    if (a.segments > 1) {
+        a.summary = 1;
+        if (cudaLaunchKernelEx(&cfg, kern, a) != cudaSuccess) return HLA_ERR_CUDA;
+        a.summary = 0;
+    }
     return cudaLaunchKernelEx(&cfg, kern, a) == cudaSuccess ? HLA_OK : HLA_ERR_CUDA;
 }
 
@@ -556,7 +602,14 @@ hla_status hla_scan_create(const hla_scan_config* cfg, hla_scan** out) {
     return HLA_OK;
 }
 
-hla_status hla_scan_forward(hla_scan* c, const void* x, const void* g, const void* h0, void* h, void* h_last, void* cuda_stream) {
+size_t hla_scan_workspace_bytes(const hla_scan* c) {
+    if (!c || 4 * columns_of(c) > 3ll * c->sm_count) return 0;      // too many channels for segments
+    const long long n = 3ll * c->sm_count / columns_of(c);          // (clusters of one block would leave room for as many)
+    return (size_t)((n + 1) * c->cfg.B * c->cfg.C * 8 + 255) / 256 * 256;
+}
+
+hla_status hla_scan_forward(hla_scan* c, const void* x, const void* g, const void* h0, void* h, void* h_last, void* workspace, size_t workspace_bytes,
+                            void* cuda_stream) {
     if (!c || !x || !g || !h || !aligned_elt(c, x) || !aligned_elt(c, g) || !aligned16(h) || !aligned4(h0) || !aligned4(h_last)) return HLA_ERR_INVALID_ARG;
     scan::Args a = common_args(c);
     const size_t out = dense_bytes(c), state = (size_t)c->cfg.B * c->cfg.C * 4;
@@ -569,11 +622,11 @@ hla_status hla_scan_forward(hla_scan* c, const void* x, const void* g, const voi
     a.out0 = static_cast<char*>(h);
     a.in = static_cast<const float*>(h0);
     a.last = static_cast<float*>(h_last);
-    return launch(c, pick<Fwd>(c->cfg, vectors(c, a)), c->cfg.dtype == HLA_BF16 ? scan::forward_bytes<__nv_bfloat16>() : scan::forward_bytes<float>(), a, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, pick<Fwd>(c->cfg, vectors(c, a)), c->cfg.dtype == HLA_BF16 ? scan::forward_bytes<__nv_bfloat16>() : scan::forward_bytes<float>(), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const void* h0, const void* h, const void* dh, const void* dh_last,
-                             void* dx, void* dg, void* dh0, void* cuda_stream) {
+                             void* dx, void* dg, void* dh0, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     if (!c || !g || !h || !dh || !dx || !dg || (c->cfg.convex && !x)) return HLA_ERR_INVALID_ARG;
     const void* dense[] = {h, dh, dx, dg};
     for (const void* p : dense)
@@ -605,7 +658,7 @@ hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const vo
     a.in = static_cast<const float*>(dh_last);
     a.h0 = static_cast<const float*>(h0);
     a.last = static_cast<float*>(dh0);
-    return launch(c, pick<Bwd>(c->cfg, vectors(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, pick<Bwd>(c->cfg, vectors(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_destroy(hla_scan* c) {

@@ -100,6 +100,28 @@ def test_many_pieces(B, N, C, dtype, gate, convex):
     verify(B, N, C, dtype, gate, convex)
 
 
+@pytest.mark.parametrize("B,N,C,dtype,gate,convex", [(1, 20000, 33, "bf16", "log", True), (2, 9000, 64, "bf16", "sigmoid", True), (1, 8200, 1, "f32", "log", False),
+                                                     (1, 16385, 257, "bf16", "log", False), (3, 6000, 20, "f32", "sigmoid", True)])
+@pytest.mark.parametrize("carry", [False, True])
+def test_long_sequences_of_few_channels_run_in_parts(B, N, C, dtype, gate, convex, carry):
+    assert binding.Scan(B, N, C, dtype=dtype).workspace is not None
+    verify(B, N, C, dtype, gate, convex, carry=carry, fused=C == 257)
+
+
+def test_the_state_may_stay_in_its_buffer_when_a_sequence_runs_in_parts():
+    B, N, C = 1, 30000, 64
+    x, z, h0, dl, dh = inputs(B, N, C, "bf16", "sigmoid")
+    op = binding.Scan(B, N, C, gate="sigmoid")
+    h, last = op.forward(x, z, h0=h0)
+    state = h0.clone()
+    for _ in range(3):
+        state.copy_(h0)
+        got, out = op.forward(x, z, h0=state, h_last=state)
+        assert out is state and torch.equal(got, h) and torch.equal(state, last)
+    first = op.forward(x[:, :1].expand(1, N, C).contiguous(), z, h0=h0)      # (another call on the same workspace)
+    assert torch.equal(op.forward(x, z, h0=h0)[0], h) and not torch.equal(first[0], h)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_pieces_continue_a_sequence(dtype):
     """One pass and pieces with the state handed on give the same up to the roundings of both; the state may stay in one buffer."""

@@ -200,18 +200,33 @@ def test_scan_calls_are_checked_before_launching():
     st, ctx = scan(convex=1)
     assert st == OK
     far = 1 << 20
-    fwd = lambda x=P, g=P + far, h0=None, h=P + 2 * far, last=None: lib.hla_scan_forward(ctx, x, g, h0, h, last, None)
+    fwd = lambda x=P, g=P + far, h0=None, h=P + 2 * far, last=None: lib.hla_scan_forward(ctx, x, g, h0, h, last, None, 0, None)
     assert fwd(x=None) == INVALID and fwd(h=None) == INVALID and fwd(x=P + 1) == INVALID and fwd(h=P + 2 * far + 4) == INVALID and fwd(h0=P + 2) == INVALID
     assert fwd(h=P) == INVALID and fwd(h=P + far) == INVALID                              # over an input
     assert fwd(last=P + 2 * far) == INVALID and fwd(h0=P + 2 * far + 64) == INVALID and fwd(last=P + 64) == INVALID
     assert fwd(h0=P + 3 * far, last=P + 3 * far + 16) == INVALID                          # shifted, not the same
     bwd = lambda x=P, g=P + far, h0=None, h=P + 2 * far, dh=P + 3 * far, dl=None, dx=P + 4 * far, dg=P + 5 * far, d0=None: lib.hla_scan_backward(
-        ctx, x, g, h0, h, dh, dl, dx, dg, d0, None)
+        ctx, x, g, h0, h, dh, dl, dx, dg, d0, None, 0, None)
     assert bwd(x=None) == INVALID and bwd(dg=None) == INVALID and bwd(dh=P + 3 * far + 8) == INVALID and bwd(dl=P + 1) == INVALID
     assert bwd(dx=P) == INVALID and bwd(dg=P + 2 * far) == INVALID and bwd(dg=P + 4 * far) == INVALID and bwd(dx=P + 3 * far) == INVALID
     assert bwd(d0=P + 3 * far) == INVALID and bwd(d0=P + 5 * far) == INVALID and bwd(h0=P + 4 * far) == INVALID
     lib.hla_scan_destroy(ctx)
-    assert lib.hla_scan_destroy(None) == INVALID and lib.hla_scan_forward(None, P, P, None, P, None, None) == INVALID
+    assert lib.hla_scan_destroy(None) == INVALID and lib.hla_scan_forward(None, P, P, None, P, None, None, 0, None) == INVALID
+
+
+def test_scan_in_parts_needs_its_workspace():
+    lib = b.load_library()
+    assert lib.hla_scan_workspace_bytes(None) == 0
+    st, ctx = scan(B=1, N=75600, C=64)
+    assert st == OK
+    need = lib.hla_scan_workspace_bytes(ctx)
+    far = 1 << 28
+    fwd = lambda ws, n: lib.hla_scan_forward(ctx, P, P + far, None, P + 2 * far, None, ws, n, None)
+    assert need > 0 and fwd(None, 0) == INVALID and fwd(P + 3 * far + 16, need) == INVALID and fwd(P + 3 * far, need - 1) == WORKSPACE
+    lib.hla_scan_destroy(ctx)
+    st, ctx = scan(B=2, N=75600, C=1536)
+    assert st == OK and lib.hla_scan_workspace_bytes(ctx) in (0, lib.hla_scan_workspace_bytes(ctx))
+    lib.hla_scan_destroy(ctx)
 
 
 def test_scan_binding_refuses():
