@@ -106,23 +106,28 @@ struct Stage {
 };
 static_assert(Stage<float>::kHalf * 2 == 2 * kRunOf<float> && Stage<__nv_bfloat16>::kHalf * 2 == 2 * kRunOf<__nv_bfloat16>, "two pieces a lane");
 
-// One piece: 16 bytes from global to shared memory, the first `elements` of them (the rest zeros).
-template <typename T, bool VEC>
+// 16 bytes from global to shared memory, the first `elements` of them (the rest zeros), in words of WIDE bytes (16, or 4 where rows are only
+// aligned to that).
+template <typename T, int WIDE>
 __device__ __forceinline__ void copy16(uint32_t to, const char* from, int elements) {
-    if (VEC) {
+    if (WIDE == 16) {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(elements > 0 ? 16 : 0) : "memory");
     } else {
-        constexpr int n = 16 / (int)sizeof(T);
-        uint32_t w[4] = {0, 0, 0, 0};
+        constexpr int per = 4 / (int)sizeof(T);
 #pragma unroll
-        for (int i = 0; i < n; ++i)
-            if (i < elements) {
-                if (sizeof(T) == 2) w[i / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(from)[i] << (16 * (i & 1));
-                else w[i] = reinterpret_cast<const uint32_t*>(from)[i];
-            }
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+        for (int i = 0; i < 4; ++i)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * i), "l"(elements > i * per ? from + 4 * i : from), "r"(elements > i * per ? 4 : 0) : "memory");
     }
 }
+// The same through registers, for 16-bit types whose rows are not aligned to four bytes.
+__device__ __forceinline__ uint4 gather16(const char* from, int elements) {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < elements) w[i / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(from)[i] << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void put16(uint32_t to, const uint4& w) { asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory"); }
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void arrived() {
     asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
@@ -133,29 +138,39 @@ template <> __device__ __forceinline__ uint32_t read<uint32_t>(uint32_t at) { ui
 template <> __device__ __forceinline__ P2 read<P2>(uint32_t at) { P2 r; asm volatile("ld.shared.u64 %0, [%1];" : "=l"(r) : "r"(at)); return r; }
 
 // One input of a block: where this lane's pieces are, token by token forwards (step > 0) or backwards.
-template <typename T, bool VEC>
+template <typename T, int WIDE>
 struct Input {
     using S = Stage<T>;
+    static_assert(S::kHalf == S::kRun, "the second piece of a lane belongs to the second run");
     const char* at;
     long long step;           // bytes from a token to the next one in this order
+    uint4 held[2];            // WIDE 2: between get and put
     __device__ __forceinline__ Input(const char* base, long long token0, long long step_, int lane32) : at(base + token0 * step_ + (lane32 / S::kPerRow) * step_ + (lane32 % S::kPerRow) * 16), step(step_) {}
     // Copies the tokens first + (0 .. 2 kRun - 1) of the warp; tokens at `end` or behind are zeros, channels behind the last too.
     __device__ __forceinline__ void fetch(uint32_t to, int first, int end, int channels, int lane32, int stride) {
         const int row = lane32 / S::kPerRow, col = lane32 % S::kPerRow;
-        static_assert(S::kHalf == S::kRun, "the second piece of a lane belongs to the second run");
         to += row * S::kRowBytes + col * 16;
-        if (VEC && first + 2 * S::kRun <= end && channels >= kTile) {
-            copy16<T, true>(to, at, 16);
-            copy16<T, true>(to + S::kRunBytes, at + S::kHalf * step, 16);
+        if (WIDE == 16 && first + 2 * S::kRun <= end && channels >= kTile) {
+            copy16<T, 16>(to, at, 16);
+            copy16<T, 16>(to + S::kRunBytes, at + S::kHalf * step, 16);
         } else {
             const int left = channels - col * (16 / (int)sizeof(T));
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const bool in = first + row + i * S::kHalf < end;
-                copy16<T, VEC>(to + i * S::kRunBytes, in && left > 0 ? at + i * S::kHalf * step : at, in ? left : 0);
+                const bool in = first + row + i * S::kHalf < end && left > 0;
+                const char* from = in ? at + i * S::kHalf * step : at;
+                if (WIDE == 2) held[i] = gather16(from, in ? left : 0);
+                else copy16<T, WIDE>(to + i * S::kRunBytes, from, in ? left : 0);
             }
         }
         at += stride * step;
+    }
+    // WIDE 2: what fetch has read goes into shared memory (behind the fetches of the other inputs, so that their latencies are one).
+    __device__ __forceinline__ void put(uint32_t to, int lane32) {
+        if (WIDE != 2) return;
+        to += lane32 / S::kPerRow * S::kRowBytes + lane32 % S::kPerRow * 16;
+        put16(to, held[0]);
+        put16(to + S::kRunBytes, held[1]);
     }
 };
 
@@ -303,9 +318,10 @@ __device__ __forceinline__ void exchange_warp(Exchange& e, const Args& p, int ra
     }
 }
 
-template <typename T, int GATE, bool CONVEX, bool VEC>
+template <typename T, int GATE, bool CONVEX, int WIDE>
 __global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_constant__ Args p) {
     using V = Two<T>;
+    constexpr bool VEC = WIDE >= 2 * (int)sizeof(T);      // two channels of the outputs are one word
     using S = Stage<T>;
     constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>, kInputs = 2, kStages = 3;
     __shared__ Exchange e;
@@ -318,7 +334,7 @@ __global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_
     const long long gs = p.g_token * (int)sizeof(T), xs = p.x_token * (int)sizeof(T), os = (long long)p.C * (int)sizeof(T);
     const int stride = blocks * kPiece, tile = (int)blockIdx.y * kTile;
     int w0 = segment * p.pieces * stride + rank * kPiece + warp * 2 * kRun, t0 = w0 + late * kRun;      // first token of the warp, of the thread
-    Input<T, VEC> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T), w0, gs, lane32), x(p.x + (b * p.x_batch + tile) * (int)sizeof(T), w0, xs, lane32);
+    Input<T, WIDE> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T), w0, gs, lane32), x(p.x + (b * p.x_batch + tile) * (int)sizeof(T), w0, xs, lane32);
     char* po = p.out0 + ((long long)b * p.N * p.C + c) * (int)sizeof(T) + t0 * os;
     const uint32_t mine = tc::smem_u32(staged) + warp * (kStages * kInputs * S::kBytes), own = late * S::kRunBytes + lane * 2 * (int)sizeof(T);
     auto fetch = [&](int piece, int stage) {
@@ -326,6 +342,8 @@ __global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_
             const uint32_t to = mine + stage * (kInputs * S::kBytes);
             g.fetch(to, w0 + piece * stride, p.N, channels, lane32, stride);
             x.fetch(to + S::kBytes, w0 + piece * stride, p.N, channels, lane32, stride);
+            g.put(to, lane32);
+            x.put(to + S::kBytes, lane32);
         }
         commit();
     };
@@ -388,9 +406,10 @@ __global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_
 }
 
 // Tokens are counted from the end: i = N - 1 - t; pointers go down.
-template <typename T, int GATE, bool CONVEX, bool VEC>
+template <typename T, int GATE, bool CONVEX, int WIDE>
 __global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid_constant__ Args p) {
     using V = Two<T>;
+    constexpr bool VEC = WIDE >= 2 * (int)sizeof(T);      // two channels of the outputs are one word
     using Raw = typename V::Raw;
     using S = Stage<T>;
     constexpr int kRun = kRunOf<T>, kPiece = kPieceOf<T>, kInputs = CONVEX ? 4 : 3, kStages = 2;
@@ -406,7 +425,7 @@ __global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid
     const int stride = blocks * kPiece, tile = (int)blockIdx.y * kTile;
     int w0 = segment * p.pieces * stride + rank * kPiece + warp * 2 * kRun, i0 = w0 + late * kRun;
     const long long dense = ((long long)b * p.N * p.C + tile) * (int)sizeof(T), end = p.N - 1;
-    Input<T, VEC> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T) + end * gs, w0, -gs, lane32), d(p.dh + dense + end * os, w0, -os, lane32),
+    Input<T, WIDE> g(p.g + (b * p.g_batch + tile) * (int)sizeof(T) + end * gs, w0, -gs, lane32), d(p.dh + dense + end * os, w0, -os, lane32),
         h(p.h + dense + (end - 1) * os, w0, -os, lane32), x(CONVEX ? p.x + (b * p.x_batch + tile) * (int)sizeof(T) + end * xs : nullptr, w0, -xs, lane32);
     const long long out = dense + 2 * lane * (int)sizeof(T) + (end - i0) * os;
     char *po0 = p.out0 + out, *po1 = p.out1 + out;
@@ -419,6 +438,10 @@ __global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid
             d.fetch(to + S::kBytes, first, p.N, channels, lane32, stride);
             if (!p.summary) h.fetch(to + 2 * S::kBytes, first, p.N - 1, channels, lane32, stride);      // (the state before token 0 is h0)
             if (CONVEX && !p.summary) x.fetch(to + 3 * S::kBytes, first, p.N, channels, lane32, stride);
+            g.put(to, lane32);
+            d.put(to + S::kBytes, lane32);
+            if (!p.summary) h.put(to + 2 * S::kBytes, lane32);
+            if (CONVEX && !p.summary) x.put(to + 3 * S::kBytes, lane32);
         }
         commit();
     };
@@ -489,19 +512,19 @@ namespace {
 
 using Kernel = void (*)(scan::Args);
 
-template <template <typename, int, bool, bool> class K, typename T, bool VEC>
+template <template <typename, int, bool, int> class K, typename T, int WIDE>
 Kernel pick_of(bool sigmoid, bool convex) {
-    if (sigmoid) return convex ? K<T, scan::kSigmoid, true, VEC>::get() : K<T, scan::kSigmoid, false, VEC>::get();
-    return convex ? K<T, scan::kLog, true, VEC>::get() : K<T, scan::kLog, false, VEC>::get();
+    if (sigmoid) return convex ? K<T, scan::kSigmoid, true, WIDE>::get() : K<T, scan::kSigmoid, false, WIDE>::get();
+    return convex ? K<T, scan::kLog, true, WIDE>::get() : K<T, scan::kLog, false, WIDE>::get();
 }
-template <template <typename, int, bool, bool> class K>
-Kernel pick(const hla_scan_config& c, bool vec) {
+template <template <typename, int, bool, int> class K>
+Kernel pick(const hla_scan_config& c, int wide) {
     const bool s = c.gate == HLA_GATE_SIGMOID, v = c.convex;
-    if (c.dtype == HLA_BF16) return vec ? pick_of<K, __nv_bfloat16, true>(s, v) : pick_of<K, __nv_bfloat16, false>(s, v);
-    return vec ? pick_of<K, float, true>(s, v) : pick_of<K, float, false>(s, v);
+    if (c.dtype == HLA_F32) return wide == 16 ? pick_of<K, float, 16>(s, v) : pick_of<K, float, 4>(s, v);
+    return wide == 16 ? pick_of<K, __nv_bfloat16, 16>(s, v) : wide == 4 ? pick_of<K, __nv_bfloat16, 4>(s, v) : pick_of<K, __nv_bfloat16, 2>(s, v);
 }
-template <typename T, int GATE, bool CONVEX, bool VEC> struct Fwd { static Kernel get() { return scan::forward_kernel<T, GATE, CONVEX, VEC>; } };
-template <typename T, int GATE, bool CONVEX, bool VEC> struct Bwd { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX, VEC>; } };
+template <typename T, int GATE, bool CONVEX, int WIDE> struct Fwd { static Kernel get() { return scan::forward_kernel<T, GATE, CONVEX, WIDE>; } };
+template <typename T, int GATE, bool CONVEX, int WIDE> struct Bwd { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX, WIDE>; } };
 
 int elt_size(int dtype) { return dtype == HLA_BF16 ? 2 : 4; }
 
@@ -517,11 +540,12 @@ scan::Args common_args(const hla_scan* c) {
     return a;
 }
 
-// Whether rows consist of aligned 16-byte pieces everywhere: then they are copied asynchronously; else element by element.  (The dense tensors'
-// rows, C elements, are told by C.)
-bool vectors(const hla_scan* c, const scan::Args& a) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.g);
-    return !((a.C | a.x_batch | a.x_token | a.g_batch | a.g_token) * elt_size(c->cfg.dtype) & 15) && at % 16 == 0;
+// The words in which rows can be copied: 16 bytes where all rows are aligned to that, else 4, else (16-bit types, odd rows) 2.  (The dense
+// tensors' rows, C elements, are told by C.)
+int width(const hla_scan* c, const scan::Args& a) {
+    const long long at = (long long)(reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.g));
+    const long long bits = (a.C | a.x_batch | a.x_token | a.g_batch | a.g_token) * elt_size(c->cfg.dtype) | at;
+    return !(bits & 15) ? 16 : !(bits & 3) ? 4 : 2;
 }
 
 long long columns_of(const hla_scan* c) { return (long long)((c->cfg.C + scan::kTile - 1) / scan::kTile) * c->cfg.B; }
@@ -622,7 +646,7 @@ hla_status hla_scan_forward(hla_scan* c, const void* x, const void* g, const voi
     a.out0 = static_cast<char*>(h);
     a.in = static_cast<const float*>(h0);
     a.last = static_cast<float*>(h_last);
-    return launch(c, pick<Fwd>(c->cfg, vectors(c, a)), c->cfg.dtype == HLA_BF16 ? scan::forward_bytes<__nv_bfloat16>() : scan::forward_bytes<float>(), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, pick<Fwd>(c->cfg, width(c, a)), c->cfg.dtype == HLA_BF16 ? scan::forward_bytes<__nv_bfloat16>() : scan::forward_bytes<float>(), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const void* h0, const void* h, const void* dh, const void* dh_last,
@@ -658,7 +682,7 @@ hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const vo
     a.in = static_cast<const float*>(dh_last);
     a.h0 = static_cast<const float*>(h0);
     a.last = static_cast<float*>(dh0);
-    return launch(c, pick<Bwd>(c->cfg, vectors(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, pick<Bwd>(c->cfg, width(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_destroy(hla_scan* c) {
