@@ -202,45 +202,39 @@ __device__ __forceinline__ float row_max(const P2 (&v)[2]) {
     return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));      // (bits of non-negative floats are ordered like them)
 }
 
-// 448 / most times 2^-120, never above it (x / most * 448 must not pass 448): the reciprocal's error of 2^-23 is taken off.
-__device__ __forceinline__ float codes_per_unit(float most) { return reciprocal(most) * (448.f * (1.f - 0x1p-21f) * 0x1p-120f); }
-
-// Values as e4m3.  With x / scale times 2^-120 (`per` is that factor) the smallest normal e4m3 falls on the smallest normal fp32, so that one
-// addition of 20 random bits below the code's rounds normal and subnormal codes alike.  The code ends up in the top byte: integer
-// additions and shifts are what this kernel has too many of, so the shift is a product with the addition.
+// Values as e4m3.  With x / scale times 2^-120 the smallest normal e4m3 falls on the smallest normal fp32, so that one addition of 20 random bits
+// below the code's rounds normal and subnormal codes alike.  The code ends up in the top byte: integer additions and shifts are what this
+// kernel has too many of, so the shift is a product with the addition.  `per` is 448 / most, rounded: x per may pass 448 by a unit in the
+// last place, and what that could carry over into the code of no number is cut off.
+constexpr uint32_t kTop = 0x7effffffu;
 __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&w)[4]) {
     return __byte_perm(__byte_perm(w[0], w[1], 0x0073), __byte_perm(w[2], w[3], 0x0073), 0x5410);
 }
+__device__ __forceinline__ void scaled(const P2 (&x)[2], float per, float (&y)[4]) {
+    const P2 z[2] = {mul2(mul2(x[0], twice(per)), twice(0x1p-120f)), mul2(mul2(x[1], twice(per)), twice(0x1p-120f))};
+    four(z, y);
+}
 // The codes of four entries, of a moment that may be negative (low random bits) and of one that may not (high ones, and at least 1 where
 // the entry is not zero).
-__device__ __forceinline__ uint32_t codes(const P2 (&x)[2], float per, float less, const uint32_t (&bits)[4]) {
-    const P2 scaled[2] = {less == 1.f ? mul2(x[0], twice(per)) : mul2(mul2(x[0], twice(less)), twice(per)), less == 1.f ? mul2(x[1], twice(per)) : mul2(mul2(x[1], twice(less)), twice(per))};
+__device__ __forceinline__ uint32_t codes(const P2 (&x)[2], float per, const uint32_t (&bits)[4]) {
     float y[4], s[4];
-    four(scaled, y);
+    scaled(x, per, y);
     four(x, s);
     uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = (__float_as_uint(y[j]) * 16u + (bits[j] * 4096u >> 8)) | (__float_as_uint(s[j]) & 0x80000000u);      // (the sign is shifted out)
+    for (int j = 0; j < 4; ++j) w[j] = min(__float_as_uint(y[j]) * 16u + (bits[j] * 4096u >> 8), kTop) | (__float_as_uint(s[j]) & 0x80000000u);      // (the sign is shifted out)
     return top_bytes(w);
 }
-__device__ __forceinline__ uint32_t codes_positive(const P2 (&x)[2], float per, float less, const uint32_t (&bits)[4]) {
-    const P2 scaled[2] = {less == 1.f ? mul2(x[0], twice(per)) : mul2(mul2(x[0], twice(less)), twice(per)), less == 1.f ? mul2(x[1], twice(per)) : mul2(mul2(x[1], twice(less)), twice(per))};
+__device__ __forceinline__ uint32_t codes_positive(const P2 (&x)[2], float per, const uint32_t (&bits)[4]) {
     float y[4], s[4];
-    four(scaled, y);
+    scaled(x, per, y);
     four(x, s);
     uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = max(__float_as_uint(y[j]), min(__float_as_uint(s[j]), 1u << 20)) * 16u + (bits[j] >> 8);
+    for (int j = 0; j < 4; ++j) w[j] = min(max(__float_as_uint(y[j]), min(__float_as_uint(s[j]), 1u << 20)) * 16u + (bits[j] >> 8), kTop);
     return top_bytes(w);
 }
-// Rows whose factor would not be a normal number (their largest entry from 2^14 on) are made smaller first.
-__device__ __forceinline__ bool usual(float most) { return most >= kDead && most < 16384.f; }
 __device__ __forceinline__ bool held(float most) { return most >= kDead && most <= 3.402823466e38f; }
-
-// The scale of a row whose largest entry is `most`.  A row with an entry that is no number, or infinite, is no numbers throughout.
-__device__ __forceinline__ float scale_of(float most) {
-    return most < kDead ? 0.f : most <= 3.402823466e38f ? most * (1.f / 448.f) : __int_as_float(0x7fc00000);
-}
 
 // The sum of the partial sums of the squared norm, in a fixed order, to every thread.
 __device__ __forceinline__ double block_total(const double* part, int count, double* scratch) {
@@ -327,6 +321,12 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
     }
 }
 
+// A sum that is not contracted with the product before it.
+__device__ __forceinline__ P2 sum2(P2 a, P2 b) {
+    const float2 x = both(a), y = both(b);
+    return pair(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y));
+}
+
 struct Coefficients {
     float gain, b1, r1, b2, r2, eps, lr, inv1, inv2;
     uint32_t key;
@@ -382,21 +382,20 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
             P2 g[2], m[2], v[2], w[2];
             unpack<GB>(raw.g[r], g);
             unpack<PB>(raw.p[r], w);
-            float cb1 = k.b1, cb2 = k.b2;
             if (Q8) {
-                m[0] = decode2(raw.cm[r]); m[1] = decode2(raw.cm[r] >> 16);
-                v[0] = decode2(raw.cv[r]); v[1] = decode2(raw.cv[r] >> 16);
-                cb1 *= raw.sm[r];
-                cb2 *= raw.sv[r];
+                m[0] = mul2(decode2(raw.cm[r]), twice(raw.sm[r])); m[1] = mul2(decode2(raw.cm[r] >> 16), twice(raw.sm[r]));
+                v[0] = mul2(decode2(raw.cv[r]), twice(raw.sv[r])); v[1] = mul2(decode2(raw.cv[r] >> 16), twice(raw.sv[r]));
             } else {
                 unpack<false>(raw.m[r], m);
                 unpack<false>(raw.v[r], v);
             }
+            // The moments are formed in single products and sums, each rounded: what is rounded at random to 8 bits is then the same in every
+            // program that follows the formula, and so are the codes.
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 g[j] = mul2(g[j], twice(k.gain));
-                m[j] = fma2(twice(k.r1), g[j], mul2(twice(cb1), m[j]));
-                v[j] = fma2(mul2(twice(k.r2), g[j]), g[j], mul2(twice(cb2), v[j]));
+                m[j] = sum2(mul2(twice(k.b1), m[j]), mul2(twice(k.r1), g[j]));
+                v[j] = sum2(mul2(twice(k.b2), v[j]), mul2(mul2(twice(k.r2), g[j]), g[j]));
                 const float2 square = both(v[j]);
                 const float2 below = both(fma2(pair(sqrt_fast(square.x), sqrt_fast(square.y)), twice(k.inv2), twice(k.eps)));
                 const P2 quotient = mul2(m[j], pair(reciprocal(below.x), reciprocal(below.y)));
@@ -441,24 +440,23 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
                 store_f32<WHOLE>(pv, i, n, y);
             } else {
                 const float mm = row_max(m), mv = row_max(v);
+                // one reciprocal for both: even lanes take one moment's, odd lanes the other's
+                const float most = lane & 1 ? mv : mm, per = __frcp_rn(most) * 448.f;
+                const float per_m = __shfl_sync(0xffffffffu, per, 0), per_v = __shfl_sync(0xffffffffu, per, 1);
                 uint32_t qm = 0, qv = 0;
-                float em = mm * (1.f / 448.f), ev = mv * (1.f / 448.f);
-                if (usual(mm) && usual(mv)) {
-                    qm = codes(m, codes_per_unit(mm), 1.f, bits);
-                    qv = codes_positive(v, codes_per_unit(mv), 1.f, bits);
+                float scale = most * (1.f / 448.f);
+                if (held(mm) && held(mv)) {
+                    qm = codes(m, per_m, bits);
+                    qv = codes_positive(v, per_v, bits);
                 } else {
-                    const float lm = usual(mm) ? 1.f : 0x1p-114f, lv = usual(mv) ? 1.f : 0x1p-114f;
-                    if (held(mm)) qm = codes(m, codes_per_unit(mm * lm), lm, bits);
-                    if (held(mv)) qv = codes_positive(v, codes_per_unit(mv * lv), lv, bits);
-                    em = scale_of(mm);
-                    ev = scale_of(mv);
+                    if (held(mm)) qm = codes(m, per_m, bits);
+                    if (held(mv)) qv = codes_positive(v, per_v, bits);
+                    // a row of next to nothing is zeros; one with an entry that is no number, or infinite, is no numbers throughout
+                    if (!held(most)) scale = most < kDead ? 0.f : __int_as_float(0x7fc00000);
                 }
                 store_b8<WHOLE>(pm, i, n, qm);
                 store_b8<WHOLE>(pv, i, n, qv);
-                if (lane == 0 && (WHOLE || i < n)) {
-                    pms[i / kRow] = em;
-                    pvs[i / kRow] = ev;
-                }
+                if (lane < 2 && (WHOLE || i - lane * 4 < n)) (lane ? pvs : pms)[i / kRow] = scale;
             }
         }
     };
