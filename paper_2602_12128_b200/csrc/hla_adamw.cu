@@ -35,6 +35,9 @@ constexpr int kRow = 128;                        // elements of a row: a scale o
 constexpr int kRows = 2;                         // rows of a warp per chunk
 constexpr int kChunk = kWarps * kRows * kRow;
 constexpr int kFew = 40, kMany = 360;            // tensors per launch: 3.7 and 32 KB of parameters
+// Blocks of a step on an SM.  8-bit states live on their arithmetic: three blocks with the registers for two rows side by side and the next two
+// on their way take 659 us over eight transformer blocks, four 687, two 704; one row at a time and five blocks 823.
+template <bool Q8> constexpr int kBlocks = Q8 ? 3 : 4;
 constexpr float kDead = 7.888609052210118e-31f;  // 2^-100: a row whose largest entry is below is held as zeros (its scale could not be inverted)
 
 struct Tensor {
@@ -492,7 +495,7 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
 }
 
 template <int MANY, bool Q8, bool PB, bool GB>
-__global__ void __launch_bounds__(kThreads, 4) step_kernel(const __grid_constant__ Args<MANY> a) {
+__global__ void __launch_bounds__(kThreads, kBlocks<Q8>) step_kernel(const __grid_constant__ Args<MANY> a) {
     __shared__ double scratch[kWarps];
     __shared__ float hyper[2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -582,7 +585,7 @@ int span(const hla_adamw* c, int from, int n) {
     long long chunks = 0;
     for (int i = 0; i < n; ++i) chunks += (c->t[from + i].n + adamw::kChunk - 1) / adamw::kChunk;
     int s = 1;
-    while (s < 8 && chunks >= 2ll * s * 16 * 4 * c->sm_count) s *= 2;
+    while (s < 8 && chunks >= 2ll * s * 16 * adamw::kBlocks<false> * c->sm_count) s *= 2;
     return s;
 }
 
@@ -658,7 +661,7 @@ hla_status step(const hla_adamw* c, const hla_adamw_step_args& s, double* part, 
     for (int from = 0; from < total; from += batch(c, from)) {
         fill(a, c, from, batch(c, from));
         if (from) a.norm_out = nullptr;
-        const dim3 blocks(std::min<uint32_t>(a.units, 4u * c->sm_count));
+        const dim3 blocks(std::min<uint32_t>(a.units, (k.state == HLA_STATE_Q8 ? adamw::kBlocks<true> : adamw::kBlocks<false>) * (uint32_t)c->sm_count));
         if (!launch_step(k.state == HLA_STATE_Q8 ? step_of<MANY, true>(c->t[from]) : step_of<MANY, false>(c->t[from]), blocks, a, st)) return HLA_ERR_CUDA;
     }
     return HLA_OK;

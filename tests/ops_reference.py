@@ -83,6 +83,41 @@ def adamw(p, g, m, v, lr, t, b1=0.9, b2=0.999, eps=1e-8, wd=0.0):
     return p - lr * wd * p - lr * (m / (1 - b1 ** t)) / (torch.sqrt(v / (1 - b2 ** t)) + eps), m, v
 
 
+def mix32(x):
+    x = x ^ (x >> 16)
+    x = x * 0x7FEB352D & 0xFFFFFFFF
+    x = x ^ (x >> 15)
+    x = x * 0x846CA68B & 0xFFFFFFFF
+    return x ^ (x >> 16)
+
+
+def random_words(n, tensor, step, seed, device):
+    """The 32 random bits of each element of a tensor in a step."""
+    M = 0xFFFFFFFF
+    k = mix32((mix32(mix32(mix32(seed & M) ^ seed >> 32) ^ step & M) + tensor) & M)
+    i = torch.arange(0, n, 2, dtype=torch.int64, device=device)
+    x = mix32((k + i // 128 * 0x9E3779B9) & M) + i % 128 // 2 * 0x9E3779B9 & M
+    x = (x ^ x >> 16) * 0x7FEB352D & M
+    x = (x ^ x >> 15) * 0x846CA68B & M
+    y = x * 0xC2B2AE35 & M
+    return torch.stack([x ^ x >> 16, y ^ y >> 15], -1).view(-1)[:n]
+
+
+def round_q8(x, bits20):
+    """Codes (as signed magnitudes in units of the code) and scales of x, rounded by 20 random bits: the code below, or the one above where the
+    random number is within the remainder.  In 64 bits, from the products in 32 that the formula names."""
+    n = x.numel()
+    rows = torch.nn.functional.pad(x, (0, -n % 128)).view(-1, 128)
+    most = rows.abs().amax(1)
+    y = (rows * (most.reciprocal() * 448.0)[:, None]).view(-1)[:n].abs().double()
+    binade = torch.frexp(y.clamp_min(2.0 ** -6))[1].to(torch.int64) - 1
+    step = (binade - 3 + 1023 << 52).view(torch.float64)                 # (powers of two by their bits: 2.0 ** x is off by a unit on the GPU)
+    below = torch.floor(y / step)
+    up = ((y / step - below) * 2 ** 20).floor() + bits20 >= 2 ** 20
+    value = torch.where(y > 0, ((below + up) * step).clamp_max(448.0), 0.0)
+    return value * torch.where(x < 0, -1.0, 1.0), most * (1.0 / torch.tensor(448.0, device=x.device))
+
+
 def decode_q8(codes, scales):
     n = codes.numel()
     return codes.view(torch.float8_e4m3fn).double() * scales.double().repeat_interleave(128)[:n]

@@ -171,6 +171,31 @@ def test_gradients_of_any_size(size):
     assert torch.isfinite(opt.m_scales[0]).all() and torch.isfinite(opt.v_scales[0]).all()
 
 
+def test_codes_are_those_of_the_formula():
+    """Three steps of 8-bit states on several tensors: every code and scale is what moments formed in single rounded products and sums and the random
+    numbers of (seed, step, tensor, element) give, so that another program can follow.  (Below the normal codes a value is first rounded to 2^-20 of
+    a step, which the reference does not: one of a million may go the other way.)"""
+    sizes, seed = [6, 130, 5000, 128 * 77], 0x123456789AB
+    ps, gs, ms, vs = tensors(sizes, torch.bfloat16, torch.bfloat16)
+    (ms, msc), (vs, vsc) = (map(list, zip(*[quantise(x) for x in xs])) for xs in (ms, vs))
+    opt = binding.AdamW(ps, gs, ms, vs, m_scales=msc, v_scales=vsc, seed=seed)
+    f = lambda v: torch.tensor(v, dtype=torch.float32, device="cuda")
+    for step in (7, 8, 2**33 + 1):
+        held = [(ref.decode_q8(m, a).float(), ref.decode_q8(v, b).float()) for m, v, a, b in zip(ms, vs, msc, vsc)]
+        opt.step(1e-3, step)
+        for i, n in enumerate(sizes):
+            g = gs[i].float()
+            m = f(0.9) * held[i][0] + f(1 - 0.9) * g
+            v = f(0.999) * held[i][1] + f(1 - 0.999) * g * g
+            bits = ref.random_words(n, i, step, seed, "cuda")
+            for x, low, codes, scale in ((m, bits & 0xFFFFF, ms[i], msc[i]), (v, bits >> 12, vs[i], vsc[i])):
+                want, scales = ref.round_q8(x, low)
+                if x is v:
+                    want = torch.where(v > 0, want.clamp_min(2.0 ** -9), want)
+                assert torch.equal(scale, scales)
+                assert (codes.view(torch.float8_e4m3fn).double() != want).sum() <= 1
+
+
 def test_rounding_keeps_the_mean():
     """Steps of 8-bit moments and bf16 weights are rounded so that their mean is kept: the mean error of n independent roundings,
     each within one step and of variance at most a quarter step squared, is within five standard deviations of zero."""
