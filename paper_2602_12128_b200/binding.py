@@ -521,6 +521,17 @@ class _Maker:
 class _Owner:
     """Holds a context of the library until it is closed or collected."""
     ctx, _destroy = None, ""
+    workspace, _scratch, _need, _on = None, 0, 0, -1
+
+    def _make_workspace(self, name, device):
+        self._need = int(getattr(load_library(), name)(self.ctx))
+        if device and self._need:
+            self.workspace = torch.empty(self._need, dtype=torch.uint8, device=device)
+            self._scratch, self._on = self.workspace.data_ptr(), self.workspace.get_device()
+
+    def _workspace_here(self, device):
+        if self._on not in (-1, device):
+            raise ValueError(f"the workspace is on {self.workspace.device}, but the current device is cuda:{device}")
 
     def close(self):
         if self.ctx:
@@ -571,9 +582,7 @@ class Heads(_Owner):
         self._rows, self._out, self._weight = torch.Size((B, N, H, d)), torch.Size((B, H, N, d)), torch.Size((d,))
         self._places = {2: (torch.Size((N, len(axes))), 0), 3: (torch.Size((B, N, len(axes))), N * len(axes))}
         self._new, self._new_dw = _Maker(self._out, self.torch_dtype, device), _Maker(self._weight, torch.float32, device)
-        self._need = int(load_library().hla_heads_workspace_bytes(self.ctx))
-        self.workspace = torch.empty(self._need, dtype=torch.uint8, device=device) if device and self._need else None
-        self._scratch = _ptr(self.workspace)
+        self._make_workspace("hla_heads_workspace_bytes", device)
         rows = [HlaRows() for _ in range(6)]
         self._slots = [(what, r, byref(r)) for what, r in zip(("q", "k", "v", "dq", "dk", "dv"), rows)]
         self._forward, self._backward = load_library().hla_heads_forward, load_library().hla_heads_backward
@@ -620,6 +629,7 @@ class Heads(_Owner):
         """Writes the gradients of q, k, v into dq, dk, dv (views [B,N,H,d]; only where dQ, dK, dV are given) and returns those of the norm
         weights (fp32 [d]; None without norm).  v is accepted next to q and k and not read."""
         dt, dev, f32 = self.torch_dtype, _device(), torch.float32
+        self._workspace_here(dev)
         norm = self.cfg.norm == 1
         x = [self._strided(t, i, dev) if norm and t is not None else None for i, t in enumerate((q, k))]
         out = [self._strided(t, 3 + i, dev) if t is not None else None for i, t in enumerate((dq, dk, dv))]
@@ -680,11 +690,11 @@ class AdamW(_Owner):
         cfg = HlaAdamwConfig(betas[0], betas[1], eps, HLA_STATE_Q8 if q8 else HLA_STATE_F32, seed)
         self.ctx = _create("hla_adamw_create", byref(cfg), rows, n)
         # the library only borrows pointers
-        self.params, self.grads, self.ms, self.vs, self.m_scales, self.v_scales, self.copies = params, grads, ms, vs, m_scales, v_scales, copies
+        keep = lambda v: None if v is None else list(v)  # noqa: E731
+        self.params, self.grads, self.ms, self.vs, self.m_scales, self.v_scales, self.copies = map(keep, (params, grads, ms, vs, m_scales, v_scales, copies))
         self.steps = 0
-        self._need = int(load_library().hla_adamw_workspace_bytes(self.ctx))
-        self.workspace = torch.empty(self._need, dtype=torch.uint8, device=device)
-        self._scratch, self._on, self._norm = self.workspace.data_ptr(), self.norm.get_device(), self.norm.data_ptr()
+        self._make_workspace("hla_adamw_workspace_bytes", self.norm.device)
+        self._on, self._norm = self.norm.get_device(), self.norm.data_ptr()
         self._step = load_library().hla_adamw_step
 
     @staticmethod
@@ -701,7 +711,7 @@ class AdamW(_Owner):
         st = load_library().hla_adamw_set_grads(self.ctx, (c_void_p * len(grads))(*[g.data_ptr() for g in grads]), len(grads))
         if st != HLA_OK:
             raise HlaError(st, "hla_adamw_set_grads")
-        self.grads = grads
+        self.grads = list(grads)
 
     def step(self, lr, step=None, max_norm=0.0, grad_scale=1.0, stream=None):
         """lr: a number, or an fp32 CUDA scalar that the step reads.  step: its number from 1 on (None: counted here), or an int64 CUDA scalar: with
@@ -718,7 +728,7 @@ class AdamW(_Owner):
         else:
             a.step = self.steps + 1 if step is None else step
         if self._on != _device():
-            raise ValueError(f"the tensors are on {self.workspace.device}, but the current device is cuda:{_device()}")
+            raise ValueError(f"the tensors are on cuda:{self._on}, but the current device is cuda:{_device()}")
         st = self._step(self.ctx, byref(a), self._scratch, self._need, _stream(stream))
         if st != HLA_OK:
             raise HlaError(st, "hla_adamw_step")
@@ -741,9 +751,7 @@ class Scan(_Owner):
         self.device = device
         self._shape, self._state = torch.Size((B, N, C)), torch.Size((B, C))
         self._new, self._new_state = _Maker(self._shape, self.torch_dtype, device), _Maker(self._state, torch.float32, device)
-        self._need = int(load_library().hla_scan_workspace_bytes(self.ctx))
-        self.workspace = torch.empty(self._need, dtype=torch.uint8, device=device) if device and self._need else None
-        self._scratch = _ptr(self.workspace)
+        self._make_workspace("hla_scan_workspace_bytes", device)
         self._forward, self._backward = load_library().hla_scan_forward, load_library().hla_scan_backward
 
     def _make(self):
@@ -756,6 +764,7 @@ class Scan(_Owner):
         _here(x, "x", self.torch_dtype, self._shape, device)
         _here(g, "g", self.torch_dtype, self._shape, device)
         strides = x.stride(), g.stride()
+        self._workspace_here(device)
         if strides == self._seen:
             return
         B, N, C = self._shape

@@ -678,6 +678,7 @@ hla_status hla_adamw_create(const hla_adamw_config* cfg, const hla_adamw_tensor*
         return HLA_ERR_INVALID_ARG;
     if (cfg->state != HLA_STATE_F32 && cfg->state != HLA_STATE_Q8) return HLA_ERR_INVALID_ARG;
     const bool q8 = cfg->state == HLA_STATE_Q8;
+    if (q8 && cfg->eps < 0x1p-50) return HLA_ERR_INVALID_ARG;      // a row of second moments below 2^-100 is held as zeros: eps has to cover their roots
     if (n > (1 << 20)) return HLA_ERR_UNSUPPORTED;
     try {
         std::unique_ptr<hla_adamw> c(new hla_adamw());

@@ -474,7 +474,7 @@ int heads_per_run(const hla_heads* c, int tensors) {
     const long long tokens = (long long)c->cfg.B * c->cfg.N;
     const int groups = heads::kThreads >> c->log_lanes;
     int chunks = 1;
-    while (chunks < c->cfg.H && tokens * tensors * chunks < 4ll * c->sm_count * groups) chunks *= 2;
+    while (chunks < c->cfg.H && chunks < 16384 && tokens * tensors * chunks < 4ll * c->sm_count * groups) chunks *= 2;      // (a grid has 65535 rows of blocks)
     if (chunks > c->cfg.H) chunks = c->cfg.H;
     return (c->cfg.H + chunks - 1) / chunks;
 }

@@ -294,27 +294,31 @@ __device__ __forceinline__ void start(Exchange& e) {
     cluster_sync();
 }
 
-// The exchanging warp of a block: its state going in, through the maps of the segments before its own, and out.
-__device__ __forceinline__ void exchange_warp(Exchange& e, const Args& p, int rank, int blocks, int b, int segment) {
+// The state that goes into this block's part of a channel (the exchanging warp's lane), through the maps of the segments before its own.  Read
+// before the cluster's first barrier: the state that goes out may lie over it.  (With segments, which end in any order, its copy from the first
+// pass is read.)
+__device__ __forceinline__ float state_in(const Args& p, int b, int segment) {
     const int c = blockIdx.y * kTile + (threadIdx.x & 31);
-    const bool live = c < p.C;
+    if (p.summary || threadIdx.x < kThreads || c >= p.C) return 0.f;
     const size_t at = (size_t)b * p.C + c, all = (size_t)(gridDim.z / p.segments) * p.C;
     float carry = 0.f;
-    if (!p.summary && live) {
-        // (the state that goes out may lie over the one that comes in: with segments, which end in any order, its copy from the first pass is read)
-        if (p.in) carry = p.segments > 1 ? p.maps[p.segments * all + at].x : p.in[at];
-        for (int i = 0; i < segment; ++i) {
-            const float2 m = p.maps[i * all + at];
-            carry = fmaf(m.x, carry, m.y);
-        }
+    if (p.in) carry = p.segments > 1 ? p.maps[p.segments * all + at].x : p.in[at];
+    for (int i = 0; i < segment; ++i) {
+        const float2 m = p.maps[i * all + at];
+        carry = fmaf(m.x, carry, m.y);
     }
+    return carry;
+}
+__device__ __forceinline__ void exchange_warp(Exchange& e, const Args& p, int rank, int blocks, int b, int segment, float carry) {
+    const int c = blockIdx.y * kTile + (threadIdx.x & 31);
+    const size_t at = (size_t)b * p.C + c, all = (size_t)(gridDim.z / p.segments) * p.C;
     const float2 map = exchange(e, p.pieces, rank, blocks, carry);
-    if (rank == 0 && live) {
-        if (p.summary) {
-            p.maps[segment * all + at] = map;
-            if (segment == 0 && p.in) p.maps[p.segments * all + at] = make_float2(p.in[at], 0.f);
-        }
-        else if (p.last && segment == p.segments - 1) p.last[at] = map.y;
+    if (rank != 0 || c >= p.C) return;
+    if (p.summary) {
+        p.maps[segment * all + at] = map;
+        if (segment == 0 && p.in) p.maps[p.segments * all + at] = make_float2(p.in[at], 0.f);
+    } else if (p.last && segment == p.segments - 1) {
+        p.last[at] = map.y;
     }
 }
 
@@ -351,9 +355,10 @@ __global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_
 #pragma unroll
         for (int i = 0; i < kStages; ++i) fetch(i, i);
     }
+    const float carry = state_in(p, b, segment);
     start(e);
     if (warp == kThreads / 32) {
-        exchange_warp(e, p, rank, blocks, b, segment);
+        exchange_warp(e, p, rank, blocks, b, segment, carry);
         cluster_sync();      // no block leaves while another may still write into its shared memory
         return;
     }
@@ -449,9 +454,10 @@ __global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid
 #pragma unroll
         for (int i = 0; i < kStages; ++i) fetch(i, i);
     }
+    const float carry = state_in(p, b, segment);
     start(e);
     if (warp == kThreads / 32) {
-        exchange_warp(e, p, rank, blocks, b, segment);
+        exchange_warp(e, p, rank, blocks, b, segment, carry);
         cluster_sync();      // no block leaves while another may still write into its shared memory
         return;
     }

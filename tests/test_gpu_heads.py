@@ -211,6 +211,13 @@ def test_repeats_streams_and_graphs():
     assert all(torch.equal(a, b) for a, b in zip(got, new)) and not torch.equal(new[0], want[0])
 
 
+def test_very_many_heads_of_one_token():
+    """More runs of heads than a grid has rows of blocks."""
+    H = 60000
+    op, xs, ws, ds = make(1, H, (1, 1, 1), 8, "bf16", (4, 2, 2))
+    verify(op, xs, ws, ds, ref.angles(ref.grid_positions((1, 1, 1)), (4, 2, 2)), "interleaved", True, 1.0, "bf16", (4, 2, 2))
+
+
 @pytest.mark.parametrize("H,grid,d,dtype", [(24, (5, 39, 40), 128, "bf16"), (5, (7, 30, 31), 64, "f32")])
 def test_longer_sequences(H, grid, d, dtype):
     axes = {128: (44, 42, 42), 64: (24, 20, 20)}[d]

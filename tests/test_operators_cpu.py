@@ -130,7 +130,7 @@ def tensor(at=P, n=100, **kw):
     ([tensor(m_scale=0)], {}, OK), ([tensor(m_scale=0)], dict(state=1), INVALID), ([tensor(v_scale=P + 4)], dict(state=1), INVALID),
     ([tensor(param_dtype=2)], {}, INVALID), ([tensor(grad_dtype=-1)], {}, INVALID), ([tensor(copy=P + (6 << 16), param_dtype=b.HLA_BF16)], {}, INVALID),
     ([tensor(lr_mul=float("nan"))], {}, INVALID), ([tensor(weight_decay=float("inf"))], {}, INVALID),
-    ([tensor()], dict(beta1=1.0), INVALID), ([tensor()], dict(beta2=-0.1), INVALID), ([tensor()], dict(eps=0.0), INVALID), ([tensor()], dict(eps=1e-60), INVALID),
+    ([tensor()], dict(beta1=1.0), INVALID), ([tensor()], dict(beta2=-0.1), INVALID), ([tensor()], dict(eps=0.0), INVALID), ([tensor()], dict(eps=1e-60), INVALID), ([tensor()], dict(eps=1e-16, state=1), INVALID), ([tensor()], dict(eps=1e-16), OK),
     ([tensor()], dict(state=2), INVALID), ([tensor()], dict(beta1=float("nan")), INVALID),
     ([tensor(), tensor()], {}, INVALID),                                                   # the same tensor twice
     ([tensor(), tensor(P + (1 << 20), m=P + 384)], {}, INVALID),                           # a moment over the end of another's weights
