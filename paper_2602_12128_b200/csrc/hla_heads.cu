@@ -214,18 +214,22 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
     const char* src = t.x + b * t.x_batch + n * t.x_token + h0 * row;
     char* dst = t.out + ((size_t)b * p.H + h0) * head + n * row;
 
+    uint4 r[U];
+    auto fetch = [&](int h) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            r[u] = make_uint4(0, 0, 0, 0);
+            if (mine && h + u < count) r[u] = at.load(src + u * row);
+        }
+    };
+    fetch(0);      // (on their way while the angles are computed)
     P2 c[NQ], s[NQ], wa[NQ], wb[NQ];
     if (t.rotate) {
         angles<T, HALF>(p, turns, l, b, n, t.scale, c, s);
         if (NORM) norm_weights<T, HALF>(t.w, at, wa, wb);
     }
     for (int h = 0; h < p.per_chunk; h += U) {
-        uint4 r[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            r[u] = make_uint4(0, 0, 0, 0);
-            if (mine && h + u < count) r[u] = at.load(src + u * row);
-        }
+        if (h) fetch(h);
         if (t.rotate) {
             float scale[U];
             if (NORM) {
