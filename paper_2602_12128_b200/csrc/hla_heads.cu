@@ -214,22 +214,29 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
     const char* src = t.x + b * t.x_batch + n * t.x_token + h0 * row;
     char* dst = t.out + ((size_t)b * p.H + h0) * head + n * row;
 
-    uint4 r[U];
+    __shared__ uint4 staged[2][U][kThreads];
     auto fetch = [&](int h) {
+        if (mine && h < count) {
+            uint4(*to)[kThreads] = staged[h / U & 1];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            r[u] = make_uint4(0, 0, 0, 0);
-            if (mine && h + u < count) r[u] = at.load(src + u * row);
+            for (int u = 0; u < U; ++u)
+                if (h + u < count) at.copy(&to[u][threadIdx.x], src + u * row);
         }
+        src += U * row;
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
     fetch(0);      // (on their way while the angles are computed)
+    fetch(U);
     P2 c[NQ], s[NQ], wa[NQ], wb[NQ];
     if (t.rotate) {
         angles<T, HALF>(p, turns, l, b, n, t.scale, c, s);
         if (NORM) norm_weights<T, HALF>(t.w, at, wa, wb);
     }
     for (int h = 0; h < p.per_chunk; h += U) {
-        if (h) fetch(h);
+        uint4 r[U];
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+#pragma unroll
+        for (int u = 0; u < U; ++u) r[u] = mine && h + u < count ? staged[h / U & 1][u][threadIdx.x] : make_uint4(0, 0, 0, 0);
         if (t.rotate) {
             float scale[U];
             if (NORM) {
@@ -271,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (mine && h + u < count) at.store(dst + u * head, r[u]);
-        src += U * row;
+        fetch(h + 2 * U);
         dst += U * head;
     }
 }
