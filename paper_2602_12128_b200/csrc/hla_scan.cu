@@ -557,19 +557,20 @@ int width(const hla_scan* c, const scan::Args& a) {
 long long columns_of(const hla_scan* c) { return (long long)((c->cfg.C + scan::kTile - 1) / scan::kTile) * c->cfg.B; }
 
 // Parts of a sequence that run side by side: a first pass finds the map of each, and the pass proper starts every part from the states that the
-// maps before it give.  It reads the inputs twice, so it is taken where at least four parts fit on the machine next to one another and each
-// still has several exchanges (75600 tokens of 64 channels: XX us in one part, YY us in 13).
+// maps before it give.  It reads the inputs twice, so it is taken where at least three parts fit on the machine next to one another (75600 tokens:
+// 64 channels 78 us in one part, 29 in 27; 512 channels backward 158 and 131 in three; 32760 tokens of 768 channels 49 and 70 in two, which
+// is not taken).
 int segments_of(const hla_scan* c, int blocks, long long pieces) {
     long long n = 3ll * c->sm_count / (blocks * columns_of(c));
     if (n > pieces / 2) n = pieces / 2;
-    return n < 4 ? 1 : (int)n;
+    return n < 3 ? 1 : (int)n;
 }
 
 hla_status launch(const hla_scan* c, Kernel kern, int bytes, scan::Args& a, void* workspace, size_t workspace_bytes, cudaStream_t st) {
     int blocks = 1;      // of a cluster
     const int piece = c->cfg.dtype == HLA_BF16 ? scan::kPieceOf<__nv_bfloat16> : scan::kPieceOf<float>;
     // as many as sequences and channels leave room for (three blocks an SM): a second wave would wait for the first, and with fewer blocks in a
-    // cluster an exchange is shorter.  Backward of 2 x 32760 tokens, 1536 channels: 8 blocks a cluster (1.7 waves) 247 us, 4 blocks 233 us
+    // cluster an exchange is shorter.  Backward of 2 x 32760 tokens, 1536 channels: 8 blocks a cluster (1.7 waves) 223 us, 4 blocks 213 us
     const long long columns = columns_of(c), room = 3ll * c->sm_count;
     while (blocks < scan::kMaxCluster && blocks * piece < a.N && 2 * blocks * columns <= room) blocks *= 2;
     const long long total = ((long long)a.N + blocks * piece - 1) / (blocks * piece);
@@ -633,7 +634,7 @@ hla_status hla_scan_create(const hla_scan_config* cfg, hla_scan** out) {
 }
 
 size_t hla_scan_workspace_bytes(const hla_scan* c) {
-    if (!c || 4 * columns_of(c) > 3ll * c->sm_count) return 0;      // too many channels for segments
+    if (!c || 3 * columns_of(c) > 3ll * c->sm_count) return 0;      // too many channels for segments
     const long long n = 3ll * c->sm_count / columns_of(c);          // (clusters of one block would leave room for as many)
     return (size_t)((n + 1) * c->cfg.B * c->cfg.C * 8 + 255) / 256 * 256;
 }
