@@ -365,8 +365,8 @@ hla_status hla_heads_create(const hla_heads_config *cfg, hla_heads **out);
 /* Scratch of hla_heads_backward (0 without norm; only needed where it is asked for dwq or dwk). */
 size_t hla_heads_workspace_bytes(const hla_heads *ctx);
 
-/* q, k, v -> Q, K, V [B][H][N][d], each may be NULL together with its output.  wq, wk: norm weights [d], NULL for ones.
- * No output may lie within the memory that an input spans. */
+/* q, k, v -> Q, K, V [B][H][N][d], each may be NULL together with its output.  wq, wk: norm weights [d] (norm = 1 only), NULL for
+ * ones.  No output may lie within the memory that an input spans. */
 hla_status hla_heads_forward(hla_heads *ctx, const hla_rows *q, const hla_rows *k, const hla_rows *v, const void *wq, const void *wk,
                              const int32_t *positions, int64_t positions_batch_stride, void *Q, void *K, void *V, void *cuda_stream);
 
@@ -410,7 +410,7 @@ typedef struct {
     int32_t param_dtype, grad_dtype; /* hla_dtype                                                      */
 } hla_adamw_tensor;
 typedef struct {
-    double beta1, beta2, eps;    /* 0 <= beta < 1, eps > 0                                             */
+    double beta1, beta2, eps;    /* 0 <= beta < 1, eps > 0 (HLA_STATE_Q8: eps >= 2^-50)                */
     int32_t state;               /* hla_state_type                                                     */
     uint64_t seed;
 } hla_adamw_config;
@@ -439,7 +439,7 @@ hla_status hla_adamw_destroy(hla_adamw *ctx);
  *     u_t = x_t, or (1 - a_t) x_t with convex = 1.
  * x, g [B][N][C] with strides (x and g may be parts of one projection); h, dh, dx, dg [B][N][C] contiguous and 16-byte aligned; states
  * h0, h_last, dh_last, dh0 are fp32 [B][C] and may be NULL (zeros; not wanted).  A sequence that arrives in pieces is continued by
- * passing the h_last of one call as the h0 of the next, the same buffer if wanted.  The state is carried in fp32, whatever the
+ * passing the h_last of one call as the h0 of the next, the same buffer if wanted (not a part of it).  The state is carried in fp32, whatever the
  * dtype.  The backward returns the gradients of sum(dh h) + sum(dh_last h_last) with respect to x, g and h0; h is the output of
  * the forward.  x is only read there with convex = 1.  Outputs may not lie over inputs, but for dh0 over h0 or dh_last.
  */

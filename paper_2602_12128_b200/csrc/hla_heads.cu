@@ -4,12 +4,14 @@
 //     g = s R(-theta_n) dy,   dw = sum g . x r,   dx = r (g . w - x r mean(g . w . x r))
 //
 // What bounds it: memory.  A row of d channels is read once (the backward: dy and x), about ten operations an element, and
-// written once, at another place: the rows of one token lie together in the projection, those of one head in Q, K, V.
+// written once, at another place: the rows of one token lie together in the projection, those of one head in Q, K, V.  Forward of
+// 24 x 32760 rows of 128 bf16 channels (q, k, v): 198 us, 6.1 TB/s; backward of twice as many 511 us, 6.3 TB/s.
 //
 // Layout: 16 bytes of a row per lane, so a row of 128 bf16 channels is half a warp and is summed with four shuffles; the two
 // channels of every pair are in the same lane in both pairings.  Such a group of lanes takes one token and goes through the
 // heads of one tensor: the angles of a token (a product and a reduction in 64 bits, one sincospi per pair) are computed once and
-// stay in registers.  Neighbouring groups take neighbouring tokens, so a block reads rows of H d and writes runs of 16 tokens.
+// stay in registers.  Neighbouring groups take neighbouring tokens, so a block reads rows of H d and writes runs of 16 tokens.  The next rows
+// of a lane are on their way through shared memory: with as many in registers the forward took 207 us.
 #include "../../include/hla.h"
 
 #include <math.h>

@@ -6,12 +6,16 @@
 // A step is the affine map h -> a h + u, and maps compose: (A2, H2) o (A1, H1) = (A2 A1, A2 H1 + H2).  The backward is the same
 // recurrence in mu (mu_t = a_t mu_{t+1} + a_t dh_t) from the last token to the first, with the rest pointwise.
 //
-// What bounds it: memory, if every input is read once.  A channel is sequential and there are too few channels to fill the machine, so a
-// sequence is cut: a thread takes two channels of kRun consecutive tokens, composes them in registers, and composes the runs before its
-// own from shared memory; a cluster of up to eight blocks takes neighbouring pieces of the sequence and hands the maps of its blocks
-// round through distributed shared memory, once for every kPiece tokens of a block.  The tokens stay in registers meanwhile and are gone
-// through once more from the state that comes in; the next piece is loaded before the exchange.  All orders are fixed: results do not
-// depend on timing.  States, maps and sums are fp32.
+// What bounds it: memory would, if every input is read once; a channel is sequential and there are too few channels to fill the machine, so
+// a sequence is cut.  A thread takes two channels of kRun consecutive tokens and composes their maps in registers; one warp of a block
+// composes those of its runs; a cluster of up to eight blocks takes neighbouring pieces of the sequence and hands the maps of its blocks
+// round through distributed shared memory, once for every kPieceOf tokens of a block.  The tokens stay in registers meanwhile and are gone
+// through once more from the state that comes in; the next pieces are on their way into shared memory.  All orders are fixed: results
+// do not depend on timing.  States, maps and sums are fp32.
+//
+// Forward of 32760 tokens, 1536 channels, bf16, sigmoid gates, convex: 73 us, 4.1 TB/s of 6.5, 24.5 instructions an element, 54 % of the issue
+// slots.  The rest is the wait for the slowest block of a cluster (384 blocks on 148 SMs: three on some, two on others) and the round through the
+// cluster.  Backward of two such sequences, log gates: 213 us, 4.7 TB/s, 40 instructions an element at 67 %.
 #include "../../include/hla.h"
 
 #include <new>
