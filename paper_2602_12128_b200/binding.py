@@ -553,6 +553,14 @@ def _create(name, *args) -> int:
     return out.value
 
 
+class _Slot:
+    """One strided argument of Heads: what it is called, the library's description of it and the strides that this has."""
+
+    def __init__(self, what):
+        self.what, self.rows, self.strides = what, HlaRows(), None
+        self.at = byref(self.rows)
+
+
 class Heads(_Owner):
     """Head preparation around a projection (hla_heads_*): RMS norm of the rows of q and k, rotation by up to three axes, scale of q, and
     the move from [B,N,H,d] (any token stride: parts of one projection) to the [B,H,N,d] that Hla takes; and its backward.
@@ -583,20 +591,24 @@ class Heads(_Owner):
         self._places = {2: (torch.Size((N, len(axes))), 0), 3: (torch.Size((B, N, len(axes))), N * len(axes))}
         self._new, self._new_dw = _Maker(self._out, self.torch_dtype, device), _Maker(self._weight, torch.float32, device)
         self._make_workspace("hla_heads_workspace_bytes", device)
-        rows = [HlaRows() for _ in range(6)]
-        self._slots = [(what, r, byref(r)) for what, r in zip(("q", "k", "v", "dq", "dk", "dv"), rows)]
+        self._slots = [_Slot(what) for what in ("q", "k", "v", "dq", "dk", "dv")]
         self._forward, self._backward = load_library().hla_heads_forward, load_library().hla_heads_backward
 
     def _strided(self, t, slot, device):
         """The tensor's place and strides for the library, in a slot of its own (reused: a context serves one call at a time)."""
-        what, row, at = self._slots[slot]
-        _here(t, what, self.torch_dtype, self._rows, device)
-        sb, sn, sh, sd = t.stride()
-        H, d = self.cfg.H, self.cfg.d
-        if (sd != 1 and d > 1) or (sh != d and H > 1):
-            raise ValueError(f"{what}: the {H} x {d} channels of a token must be contiguous")
-        row.data, row.batch_stride, row.token_stride = t.data_ptr(), sb, sn
-        return at
+        row = self._slots[slot]
+        if t.dtype is not self.torch_dtype or t.shape != self._rows or t.get_device() != device:
+            _here(t, row.what, self.torch_dtype, self._rows, device)
+        strides = t.stride()
+        if strides != row.strides:
+            sb, sn, sh, sd = strides
+            H, d = self.cfg.H, self.cfg.d
+            if (sd != 1 and d > 1) or (sh != d and H > 1):
+                raise ValueError(f"{row.what}: the {H} x {d} channels of a token must be contiguous")
+            row.rows.batch_stride, row.rows.token_stride = sb, sn
+            row.strides = strides
+        row.rows.data = t.data_ptr()
+        return row.at
 
     def _positions(self, p, device):
         if p is None:
@@ -617,9 +629,9 @@ class Heads(_Owner):
                     continue
             if outs[i] is not None:
                 at[i] = _dense(outs[i], "output", dt, shape, dev)
-        pos, pos_batch = self._positions(positions, dev)
-        st = self._forward(self.ctx, rows[0], rows[1], rows[2], _dense(wq, "wq", dt, self._weight, dev), _dense(wk, "wk", dt, self._weight, dev), pos, pos_batch,
-                           at[0], at[1], at[2], _stream(stream))
+        pos, pos_batch = self._positions(positions, dev) if positions is not None else (0, 0)
+        st = self._forward(self.ctx, rows[0], rows[1], rows[2], _dense(wq, "wq", dt, self._weight, dev) if wq is not None else 0,
+                           _dense(wk, "wk", dt, self._weight, dev) if wk is not None else 0, pos, pos_batch, at[0], at[1], at[2], _stream(stream))
         if st != HLA_OK:
             raise HlaError(st, "hla_heads_forward")
         return outs
@@ -761,8 +773,10 @@ class Scan(_Owner):
 
     def _strides(self, x, g, device):
         """Follows the strides of x and g (a context has those it was made for)."""
-        _here(x, "x", self.torch_dtype, self._shape, device)
-        _here(g, "g", self.torch_dtype, self._shape, device)
+        dt, shape = self.torch_dtype, self._shape
+        if x.dtype is not dt or x.shape != shape or x.get_device() != device or g.dtype is not dt or g.shape != shape or g.get_device() != device:
+            _here(x, "x", dt, shape, device)
+            _here(g, "g", dt, shape, device)
         strides = x.stride(), g.stride()
         self._workspace_here(device)
         if strides == self._seen:

@@ -516,6 +516,8 @@ using namespace hla;
 struct hla_scan {
     hla_scan_config cfg;
     int sm_count;
+    void (*ready[2])(scan::Args);      // forward and backward kernels that were given their shared memory, on `device`
+    int device;
 };
 
 namespace {
@@ -570,7 +572,7 @@ int segments_of(const hla_scan* c, int blocks, long long pieces) {
     return n < 3 ? 1 : (int)n;
 }
 
-hla_status launch(const hla_scan* c, Kernel kern, int bytes, scan::Args& a, void* workspace, size_t workspace_bytes, cudaStream_t st) {
+hla_status launch(hla_scan* c, bool back, Kernel kern, int bytes, scan::Args& a, void* workspace, size_t workspace_bytes, cudaStream_t st) {
     int blocks = 1;      // of a cluster
     const int piece = c->cfg.dtype == HLA_BF16 ? scan::kPieceOf<__nv_bfloat16> : scan::kPieceOf<float>;
     // as many as sequences and channels leave room for (three blocks an SM): a second wave would wait for the first, and with fewer blocks in a
@@ -591,7 +593,14 @@ hla_status launch(const hla_scan* c, Kernel kern, int bytes, scan::Args& a, void
     cfg.blockDim = dim3(scan::kThreads + 32);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return HLA_ERR_CUDA;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return HLA_ERR_CUDA;
+    if (c->ready[back] != kern || c->device != dev) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return HLA_ERR_CUDA;
+        if (c->device != dev) c->ready[!back] = nullptr;
+        c->ready[back] = kern;
+        c->device = dev;
+    }
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = blocks;
@@ -633,6 +642,7 @@ hla_status hla_scan_create(const hla_scan_config* cfg, hla_scan** out) {
     if (!x) return HLA_ERR_NO_MEMORY;
     x->cfg = c;
     x->sm_count = current_sm_count();
+    x->device = -1;
     *out = x;
     return HLA_OK;
 }
@@ -657,7 +667,7 @@ hla_status hla_scan_forward(hla_scan* c, const void* x, const void* g, const voi
     a.out0 = static_cast<char*>(h);
     a.in = static_cast<const float*>(h0);
     a.last = static_cast<float*>(h_last);
-    return launch(c, pick<Fwd>(c->cfg, width(c, a)), c->cfg.dtype == HLA_BF16 ? scan::forward_bytes<__nv_bfloat16>() : scan::forward_bytes<float>(), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, false, pick<Fwd>(c->cfg, width(c, a)), c->cfg.dtype == HLA_BF16 ? scan::forward_bytes<__nv_bfloat16>() : scan::forward_bytes<float>(), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const void* h0, const void* h, const void* dh, const void* dh_last,
@@ -693,7 +703,7 @@ hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const vo
     a.in = static_cast<const float*>(dh_last);
     a.h0 = static_cast<const float*>(h0);
     a.last = static_cast<float*>(dh0);
-    return launch(c, pick<Bwd>(c->cfg, width(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, true, pick<Bwd>(c->cfg, width(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_destroy(hla_scan* c) {
