@@ -566,7 +566,10 @@ class Heads(_Owner):
     the move from [B,N,H,d] (any token stride: parts of one projection) to the [B,H,N,d] that Hla takes; and its backward.
 
     axes: channels that turn with each axis.  grid: tokens along each axis (None: every call is given `positions`, int32 [N, axes] or
-    [B, N, axes]).  inv_freq: one value per pair (None: theta ** (-j / n) for pair j of an axis of n pairs)."""
+    [B, N, axes]).  inv_freq: one value per pair (None: theta ** (-j / n) for pair j of an axis of n pairs).
+
+    Here and in the classes below, work is enqueued on `stream` (None: the current one), tensors that a call makes belong to the current stream, and
+    the calls of one object share its workspace: they have to follow one another, in a captured graph too."""
     _destroy = "hla_heads_destroy"
 
     def __init__(self, B, H, N, d, dtype="bf16", axes=(), grid=None, start=(0, 0, 0), theta=10000.0, inv_freq=None, pairing="interleaved", norm=False,

@@ -497,8 +497,9 @@ bool rows_ok(const hla_heads* c, const hla_rows* r) {
     if (!r->data || (reinterpret_cast<uintptr_t>(r->data) & 15u)) return false;
     const long long width = (long long)c->cfg.H * c->cfg.d;
     const bool tokens = c->cfg.N > 1, batches = c->cfg.B > 1;      // a stride of one step is never taken
-    if (tokens && (r->token_stride < width || r->token_stride > (1ll << 40) || (r->token_stride * elt & 15))) return false;
-    if (batches && (r->batch_stride < (tokens ? (c->cfg.N - 1) * r->token_stride : 0) + width || r->batch_stride > (1ll << 56) || (r->batch_stride * elt & 15))) return false;
+    constexpr long long most = 1ll << 56;      // (spans are computed in 64 bits)
+    if (tokens && (r->token_stride < width || r->token_stride > most / c->cfg.N || (r->token_stride * elt & 15))) return false;
+    if (batches && (r->batch_stride < (tokens ? (c->cfg.N - 1) * r->token_stride : 0) + width || r->batch_stride > most / c->cfg.B || (r->batch_stride * elt & 15))) return false;
     return true;
 }
 

@@ -630,14 +630,14 @@ hla_status hla_scan_create(const hla_scan_config* cfg, hla_scan** out) {
     if (c.dtype != HLA_BF16 && c.dtype != HLA_F32) return HLA_ERR_INVALID_ARG;
     if (c.gate != HLA_GATE_LOG && c.gate != HLA_GATE_SIGMOID) return HLA_ERR_INVALID_ARG;
     if (c.convex != 0 && c.convex != 1) return HLA_ERR_INVALID_ARG;
-    if (c.B > 65535 || c.N > (1 << 30) || c.C > 65535 * scan::kTile) return HLA_ERR_UNSUPPORTED;
+    if (c.B > 65535 || c.N > (1 << 30) || c.C > 65535 * scan::kTile || (long long)c.B * c.N > (1ll << 48) / c.C) return HLA_ERR_UNSUPPORTED;
     if (c.x_token_stride == 0) c.x_token_stride = c.C;
     if (c.g_token_stride == 0) c.g_token_stride = c.C;
     if (c.x_batch_stride == 0) c.x_batch_stride = c.N * c.x_token_stride;
     if (c.g_batch_stride == 0) c.g_batch_stride = c.N * c.g_token_stride;
     const long long strides[4] = {c.x_token_stride, c.g_token_stride, c.x_batch_stride, c.g_batch_stride};
     for (int i = 0; i < 4; ++i)
-        if (strides[i] < c.C || strides[i] > (i < 2 ? 1ll << 30 : 1ll << 46)) return HLA_ERR_INVALID_ARG;
+        if (strides[i] < c.C || strides[i] > (1ll << 56) / (i < 2 ? c.N : c.B)) return HLA_ERR_INVALID_ARG;      // (spans are computed in 64 bits)
     hla_scan* x = new (std::nothrow) hla_scan();
     if (!x) return HLA_ERR_NO_MEMORY;
     x->cfg = c;

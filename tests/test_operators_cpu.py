@@ -58,6 +58,7 @@ def test_heads_calls_are_checked_before_launching():
     assert fwd(q=r(P + 2)) == INVALID and fwd(Q=far + 8) == INVALID
     assert fwd(q=r(token=row - 8)) == INVALID and fwd(q=r(token=row + 4)) == INVALID and fwd(q=r(batch=24 * row - 8)) == INVALID
     assert fwd(q=r(token=-row)) == INVALID and fwd(q=r(batch=0)) == INVALID
+    assert fwd(q=r(token=1 << 53)) == INVALID and fwd(q=r(batch=1 << 56)) == INVALID     # spans beyond 64 bits
     assert fwd(Q=P) == INVALID and fwd(Q=P + 2 * 24 * row * 2 - 16) == INVALID           # over its input
     assert fwd(k=r(far), K=far + (1 << 22), Q=far) == INVALID                            # Q over k
     assert fwd(v=r(far + (1 << 22)), V=far + 1024) == INVALID                            # V over Q
@@ -186,7 +187,8 @@ def scan(**kw):
 @pytest.mark.parametrize("kw,want", [
     (dict(), OK), (dict(C=1, N=1, B=1), OK), (dict(x_token_stride=81, x_batch_stride=81 * 50), OK),
     (dict(B=0), INVALID), (dict(N=-1), INVALID), (dict(C=0), INVALID), (dict(dtype=5), INVALID), (dict(gate=2), INVALID), (dict(convex=2), INVALID),
-    (dict(x_token_stride=39), INVALID), (dict(g_batch_stride=-4), INVALID), (dict(B=70000), UNSUPPORTED), (dict(N=(1 << 30) + 1), UNSUPPORTED),
+    (dict(x_token_stride=39), INVALID), (dict(g_batch_stride=-4), INVALID), (dict(B=70000), UNSUPPORTED), (dict(N=(1 << 30) + 1), UNSUPPORTED), (dict(B=60000, N=1 << 30, C=1 << 20), UNSUPPORTED),
+    (dict(x_batch_stride=1 << 57), INVALID), (dict(g_token_stride=1 << 55), INVALID), (dict(N=1 << 30, C=4, B=1, x_token_stride=1 << 40), INVALID),
 ])
 def test_scan_create(kw, want):
     st, ctx = scan(**kw)
