@@ -198,12 +198,12 @@ __device__ __forceinline__ float reciprocal(float x) {
     return r;
 }
 
-// The largest of a row's |x| from every lane's own four; not a number if one of them is none.
-__device__ __forceinline__ float row_max(const P2 (&v)[2]) {
-    float x[4];
-    four(v, x);
-    const float most = max_abs(max_abs(x[0], x[1], x[2]), x[3], x[3]);
-    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));      // (bits of non-negative floats are ordered like them)
+// The largest |x| of a lane's eight; not a number if one of them is none.
+__device__ __forceinline__ float most_of(const P2 (&v)[2][2]) {
+    float x[4], y[4];
+    four(v[0], x);
+    four(v[1], y);
+    return max_abs(max_abs(max_abs(max_abs(x[0], x[1], x[2]), x[3], y[0]), y[1], y[2]), y[3], y[3]);
 }
 
 // Values as e4m3.  With x / scale times 2^-120 the smallest normal e4m3 falls on the smallest normal fp32, so that one addition of 20 random bits
@@ -220,7 +220,7 @@ __device__ __forceinline__ void scaled(const P2 (&x)[2], float per, float (&y)[4
 }
 // The codes of four entries, of a moment that may be negative (low random bits) and of one that may not (high ones, and at least 1 where
 // the entry is not zero).
-__device__ __forceinline__ uint32_t codes(const P2 (&x)[2], float per, const uint32_t (&bits)[4]) {
+__device__ __forceinline__ uint32_t codes(const P2 (&x)[2], float per, const uint32_t* bits) {
     float y[4], s[4];
     scaled(x, per, y);
     four(x, s);
@@ -229,7 +229,7 @@ __device__ __forceinline__ uint32_t codes(const P2 (&x)[2], float per, const uin
     for (int j = 0; j < 4; ++j) w[j] = min(__float_as_uint(y[j]) * 16u + (bits[j] * 4096u >> 8), kTop) | (__float_as_uint(s[j]) & 0x80000000u);      // (the sign is shifted out)
     return top_bytes(w);
 }
-__device__ __forceinline__ uint32_t codes_positive(const P2 (&x)[2], float per, const uint32_t (&bits)[4]) {
+__device__ __forceinline__ uint32_t codes_positive(const P2 (&x)[2], float per, const uint32_t* bits) {
     float y[4], s[4];
     scaled(x, per, y);
     four(x, s);
@@ -256,11 +256,9 @@ __device__ __forceinline__ double block_total(const double* part, int count, dou
 // What a block does of a tensor in one turn: `whole` chunks, then the tensor's last, incomplete one if there is a `rest`.
 struct Share {
     long long begin;      // its first element
-    int own;              // this lane's first element from there
     int whole, rest;      // rest: elements of the incomplete chunk
-    __device__ __forceinline__ Share(const Tensor& t, uint32_t unit, int span, int warp, int lane) {
+    __device__ __forceinline__ Share(const Tensor& t, uint32_t unit, int span) {
         begin = (long long)(unit - t.first) * span * kChunk;
-        own = warp * (kRows * kRow) + lane * 4;
         const long long left = t.n - begin;
         whole = left >= (long long)span * kChunk ? span : (int)(left / kChunk);
         rest = whole < span ? (int)(left - (long long)whole * kChunk) : 0;
@@ -309,10 +307,11 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
     for (uint32_t c = blockIdx.x; c < a.units; c += gridDim.x) {
         at = tensor_of(a, c, at);
         const Tensor& t = a.t[at];
-        const Share s(t, c, a.span, warp, lane);
+        const Share s(t, c, a.span);
         const char* base = static_cast<const char*>(t.g) + s.begin * (GB ? 2 : 4);
-        if (s.whole) sum += run_squares<GB, true>(base, s.own, s.whole, 0);
-        if (s.rest) sum += run_squares<GB, false>(base + s.whole * (kChunk * (GB ? 2 : 4)), s.own, 1, s.rest);
+        const int own = warp * (kRows * kRow) + lane * 4;
+        if (s.whole) sum += run_squares<GB, true>(base, own, s.whole, 0);
+        if (s.rest) sum += run_squares<GB, false>(base + s.whole * (kChunk * (GB ? 2 : 4)), own, 1, s.rest);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -336,145 +335,213 @@ struct Coefficients {
     uint32_t key;
 };
 
-// This lane's part of `count` chunks of a tensor from element `begin` on, of `n` elements if not WHOLE.
-template <bool Q8, bool PB, bool GB, bool WHOLE>
-__device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, long long begin, int own, int count, int n, int lane) {
-    constexpr int kP = PB ? 2 : 4, kG = GB ? 2 : 4, kS = Q8 ? 1 : 4;
-    const char* pg = static_cast<const char*>(t.g) + begin * kG;
-    char *pp = static_cast<char*>(t.p) + begin * kP, *pm = static_cast<char*>(t.m) + begin * kS, *pv = static_cast<char*>(t.v) + begin * kS;
-    char* pc = PB || !t.copy ? nullptr : static_cast<char*>(t.copy) + begin * 2;
-    const uint32_t row_first = (uint32_t)(begin / kRow);      // (tensors have up to 2^38 elements)
-    float *pms = Q8 ? t.ms + row_first : nullptr, *pvs = Q8 ? t.vs + row_first : nullptr;
+// The new moments and weights of two elements.  The moments are formed in single products and sums, each rounded: what is rounded at random
+// to 8 bits is then the same in every program that follows the formula, and so are the codes.
+__device__ __forceinline__ void advance2(const Coefficients& k, float size, float shrink, P2 g, P2& m, P2& v, P2& w) {
+    g = mul2(g, twice(k.gain));
+    m = sum2(mul2(twice(k.b1), m), mul2(twice(k.r1), g));
+    v = sum2(mul2(twice(k.b2), v), mul2(mul2(twice(k.r2), g), g));
+    const float2 square = both(v);
+    const float2 below = both(fma2(pair(sqrt_fast(square.x), sqrt_fast(square.y)), twice(k.inv2), twice(k.eps)));
+    w = fma2(twice(-size), mul2(m, pair(reciprocal(below.x), reciprocal(below.y))), fma2(twice(-shrink), w, w));
+}
+
+// The random words of a row's pairs `first` to `first` + PAIRS - 1, `key` being that of its tensor.
+template <int PAIRS>
+__device__ __forceinline__ void random_words(uint32_t key, uint32_t row, int first, uint32_t (&bits)[2 * PAIRS]) {
+    const uint32_t block = mix32(key + row * 0x9E3779B9u) + (uint32_t)first * 0x9E3779B9u;
+#pragma unroll
+    for (int j = 0; j < PAIRS; ++j) {
+        uint32_t x = block + (uint32_t)j * 0x9E3779B9u;
+        x ^= x >> 16;
+        x *= 0x7FEB352Du;
+        x = (x ^ (x >> 15)) * 0x846CA68Bu;
+        const uint32_t y = x * 0xC2B2AE35u;
+        bits[2 * j] = x ^ (x >> 16);
+        bits[2 * j + 1] = y ^ (y >> 15);
+    }
+}
+
+// Four weights to bf16, rounded by the upper halves of products of their random words.
+__device__ __forceinline__ uint2 round_bf16(const float (&p)[4], const uint32_t* bits) {
+    uint32_t h[4];
+    const float any = (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h[j] = __float_as_uint(p[j]) + (bits[j] * 0x9E3779B9u >> 16);
+    if (!(fabsf(any) <= 3.402823466e38f)) {      // an infinity has no low bits to carry from; a NaN would overflow
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (p[j] != p[j]) h[j] = __float_as_uint(p[j]);
+    }
+    return make_uint2(__byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x7632));
+}
+
+// fp32 moments: `count` chunks of a tensor from element `begin` on, of `n` elements if not WHOLE.  Four elements of a row a lane.
+template <bool PB, bool GB, bool WHOLE>
+__device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, long long begin, int count, int n, int warp, int lane) {
+    constexpr int kP = PB ? 2 : 4, kG = GB ? 2 : 4;
+    const int own = warp * (kRows * kRow) + lane * 4;
+    const long long first = begin + own;
+    const char* pg = static_cast<const char*>(t.g) + first * kG;
+    char *pp = static_cast<char*>(t.p) + first * kP, *pm = static_cast<char*>(t.m) + first * 4, *pv = static_cast<char*>(t.v) + first * 4;
+    char* pc = PB || !t.copy ? nullptr : static_cast<char*>(t.copy) + first * 2;
+    uint32_t row = (uint32_t)(begin / kRow) + warp * kRows;      // (tensors have up to 2^38 elements)
     const float rate = k.lr * t.lr_mul, size = rate * k.inv1, shrink = rate * t.decay;
-    const uint32_t tensor_key = Q8 || PB ? mix32(k.key + t.number) : 0;
-    struct Raw {
-        uint4 g[kRows], p[kRows], m[kRows], v[kRows];
-        uint32_t cm[kRows], cv[kRows];
-        float sm[kRows], sv[kRows];
-    };
-    pg += own * kG;
-    pp += own * kP;
-    pm += own * kS;
-    pv += own * kS;
-    if (pc) pc += own * 2;
-    if (Q8) { pms += own / kRow; pvs += own / kRow; }
+    const uint32_t key = PB ? mix32(k.key + t.number) : 0;
     n -= own;
-    uint32_t row0 = row_first + own / kRow;
-    // the chunk that is `ahead` chunks from here
-    auto load = [&](Raw& x, int ahead) {
+    for (; count > 0; --count) {
+        uint4 rg[kRows], rp[kRows], rm[kRows], rv[kRows];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            const int i = ahead * kChunk + r * kRow;
-            x.g[r] = load_any<GB, WHOLE>(pg, i, n);
-            x.p[r] = load_any<PB, WHOLE>(pp, i, n);
-            if (Q8) {
-                const bool some = WHOLE || i - lane * 4 < n;
-                x.cm[r] = load_b8<WHOLE>(pm, i, n);
-                x.cv[r] = load_b8<WHOLE>(pv, i, n);
-                x.sm[r] = some ? pms[i / kRow] : 0.f;
-                x.sv[r] = some ? pvs[i / kRow] : 0.f;
-            } else {
-                x.m[r] = load_f32<WHOLE>(pm, i, n);
-                x.v[r] = load_f32<WHOLE>(pv, i, n);
-            }
+            const int i = r * kRow;
+            rg[r] = load_any<GB, WHOLE>(pg, i, n);
+            rp[r] = load_any<PB, WHOLE>(pp, i, n);
+            rm[r] = load_f32<WHOLE>(pm, i, n);
+            rv[r] = load_f32<WHOLE>(pv, i, n);
         }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int i = r * kRow;
+            P2 g[2], m[2], v[2], w[2];
+            unpack<GB>(rg[r], g);
+            unpack<PB>(rp[r], w);
+            unpack<false>(rm[r], m);
+            unpack<false>(rv[r], v);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) advance2(k, size, shrink, g[j], m[j], v[j], w[j]);
+            float x[4];
+            four(w, x);
+            if (PB) {
+                uint32_t bits[4];
+                random_words<2>(key, row + r, lane * 2, bits);
+                const uint2 h = round_bf16(x, bits);
+                store_bf16<WHOLE>(pp, i, n, h.x, h.y);
+            } else {
+                store_f32<WHOLE>(pp, i, n, x);
+                if (pc) store_bf16<WHOLE>(pc, i, n, two_bf16(x[0], x[1]), two_bf16(x[2], x[3]));
+            }
+            four(m, x);
+            store_f32<WHOLE>(pm, i, n, x);
+            four(v, x);
+            store_f32<WHOLE>(pv, i, n, x);
+        }
+        pg += kChunk * kG;
+        pp += kChunk * kP;
+        pm += kChunk * 4;
+        pv += kChunk * 4;
+        if (pc) pc += kChunk * 2;
+        row += kChunk / kRow;
+    }
+}
+
+// 8-bit moments, the same chunks.  Half a warp has a row, eight elements a lane: what is done once a row and lane (maximum, reciprocal, key of
+// the random numbers, addresses) is done for twice as many elements.
+template <bool PB, bool GB, bool WHOLE>
+__device__ __forceinline__ void update_q8(const Tensor& t, const Coefficients& k, long long begin, int count, int n, int warp, int lane) {
+    constexpr int kP = PB ? 2 : 4, kG = GB ? 2 : 4, kWide = 8;
+    static_assert(kRows * kRow == 32 * kWide, "two rows a warp");
+    const int own = warp * (kRows * kRow) + lane * kWide;      // (lanes 16 to 31 have the second row)
+    const long long first = begin + own;
+    const char* pg = static_cast<const char*>(t.g) + first * kG;
+    char *pp = static_cast<char*>(t.p) + first * kP, *pm = static_cast<char*>(t.m) + first, *pv = static_cast<char*>(t.v) + first;
+    char* pc = PB || !t.copy ? nullptr : static_cast<char*>(t.copy) + first * 2;
+    uint32_t row = (uint32_t)(first / kRow);
+    float *pms = t.ms + row, *pvs = t.vs + row;
+    const float rate = k.lr * t.lr_mul, size = rate * k.inv1, shrink = rate * t.decay;
+    const uint32_t key = mix32(k.key + t.number);
+    const bool second = lane & 8;      // lanes of a row whose number has this bit go by the second moment where there is one value for both
+    n -= own;
+    struct Raw {
+        uint4 g[2], p[2];      // (one each in bf16)
+        uint2 m, v;
+        float sm, sv;
+    };
+    auto load = [&](Raw& x, int ahead) {
+        const int i = ahead * kChunk;
+        if (GB && WHOLE) x.g[0] = load_f32<true>(pg + i * 2, 0, 0);      // (16 bytes)
+        else if (GB) { const uint2 lo = load_bf16<false>(pg, 0, n), hi = load_bf16<false>(pg, 4, n); x.g[0] = make_uint4(lo.x, lo.y, hi.x, hi.y); }
+        else { x.g[0] = load_f32<WHOLE>(pg, i, n); x.g[1] = load_f32<WHOLE>(pg, i + 4, n); }
+        if (PB && WHOLE) x.p[0] = load_f32<true>(pp + i * 2, 0, 0);
+        else if (PB) { const uint2 lo = load_bf16<false>(pp, 0, n), hi = load_bf16<false>(pp, 4, n); x.p[0] = make_uint4(lo.x, lo.y, hi.x, hi.y); }
+        else { x.p[0] = load_f32<WHOLE>(pp, i, n); x.p[1] = load_f32<WHOLE>(pp, i + 4, n); }
+        if (WHOLE) {
+            x.m = load_bf16<true>(pm + i, 0, 0);      // (8 bytes)
+            x.v = load_bf16<true>(pv + i, 0, 0);
+        } else {
+            x.m = make_uint2(load_b8<false>(pm, 0, n), load_b8<false>(pm, 4, n));
+            x.v = make_uint2(load_b8<false>(pv, 0, n), load_b8<false>(pv, 4, n));
+        }
+        const bool some = WHOLE || n > 0;
+        x.sm = some ? pms[i / kRow] : 0.f;
+        x.sv = some ? pvs[i / kRow] : 0.f;
     };
     auto compute = [&](const Raw& raw, int ahead) {
+        const int i = ahead * kChunk;
+        P2 g[2][2], m[2][2], v[2][2], w[2][2];      // two fours
+        if (GB) { unpack<true>(raw.g[0], g[0]); unpack<true>(make_uint4(raw.g[0].z, raw.g[0].w, 0, 0), g[1]); }
+        else { unpack<false>(raw.g[0], g[0]); unpack<false>(raw.g[1], g[1]); }
+        if (PB) { unpack<true>(raw.p[0], w[0]); unpack<true>(make_uint4(raw.p[0].z, raw.p[0].w, 0, 0), w[1]); }
+        else { unpack<false>(raw.p[0], w[0]); unpack<false>(raw.p[1], w[1]); }
+        const uint32_t cm[2] = {raw.m.x, raw.m.y}, cv[2] = {raw.v.x, raw.v.y};
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const int i = ahead * kChunk + r * kRow;
-            P2 g[2], m[2], v[2], w[2];
-            unpack<GB>(raw.g[r], g);
-            unpack<PB>(raw.p[r], w);
-            if (Q8) {
-                m[0] = mul2(decode2(raw.cm[r]), twice(raw.sm[r])); m[1] = mul2(decode2(raw.cm[r] >> 16), twice(raw.sm[r]));
-                v[0] = mul2(decode2(raw.cv[r]), twice(raw.sv[r])); v[1] = mul2(decode2(raw.cv[r] >> 16), twice(raw.sv[r]));
-            } else {
-                unpack<false>(raw.m[r], m);
-                unpack<false>(raw.v[r], v);
-            }
-            // The moments are formed in single products and sums, each rounded: what is rounded at random to 8 bits is then the same in every
-            // program that follows the formula, and so are the codes.
+        for (int f = 0; f < 2; ++f)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                g[j] = mul2(g[j], twice(k.gain));
-                m[j] = sum2(mul2(twice(k.b1), m[j]), mul2(twice(k.r1), g[j]));
-                v[j] = sum2(mul2(twice(k.b2), v[j]), mul2(mul2(twice(k.r2), g[j]), g[j]));
-                const float2 square = both(v[j]);
-                const float2 below = both(fma2(pair(sqrt_fast(square.x), sqrt_fast(square.y)), twice(k.inv2), twice(k.eps)));
-                const P2 quotient = mul2(m[j], pair(reciprocal(below.x), reciprocal(below.y)));
-                w[j] = fma2(twice(-size), quotient, fma2(twice(-shrink), w[j], w[j]));
+                m[f][j] = mul2(decode2(cm[f] >> (16 * j)), twice(raw.sm));
+                v[f][j] = mul2(decode2(cv[f] >> (16 * j)), twice(raw.sv));
+                advance2(k, size, shrink, g[f][j], m[f][j], v[f][j], w[f][j]);
             }
-            float p[4];
-            four(w, p);
-            uint32_t bits[4];
-            if (Q8 || PB) {
-                const uint32_t block = mix32(tensor_key + (row0 + ahead * (kChunk / kRow) + r) * 0x9E3779B9u) + (uint32_t)lane * 2u * 0x9E3779B9u;
+        uint32_t bits[8];
+        random_words<4>(key, row + ahead * (kChunk / kRow), (lane & 15) * 4, bits);
+        uint32_t h[4];
 #pragma unroll
-                for (int j = 0; j < 4; j += 2) {
-                    uint32_t x = block + (uint32_t)(j / 2) * 0x9E3779B9u;
-                    x ^= x >> 16;
-                    x *= 0x7FEB352Du;
-                    x = (x ^ (x >> 15)) * 0x846CA68Bu;
-                    const uint32_t y = x * 0xC2B2AE35u;
-                    bits[j] = x ^ (x >> 16);
-                    bits[j + 1] = y ^ (y >> 15);
-                }
-            }
+        for (int f = 0; f < 2; ++f) {
+            float x[4];
+            four(w[f], x);
             if (PB) {
-                uint32_t h[4];
-                const float any = (p[0] + p[1]) + (p[2] + p[3]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) h[j] = __float_as_uint(p[j]) + (bits[j] * 0x9E3779B9u >> 16);
-                if (!(fabsf(any) <= 3.402823466e38f)) {      // an infinity has no low bits to carry from; a NaN would overflow
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (p[j] != p[j]) h[j] = __float_as_uint(p[j]);
-                }
-                store_bf16<WHOLE>(pp, i, n, __byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x7632));
+                const uint2 r = round_bf16(x, bits + 4 * f);
+                h[2 * f] = r.x;
+                h[2 * f + 1] = r.y;
             } else {
-                store_f32<WHOLE>(pp, i, n, p);
-                if (pc) store_bf16<WHOLE>(pc, i, n, two_bf16(p[0], p[1]), two_bf16(p[2], p[3]));
-            }
-            if (!Q8) {
-                float x[4], y[4];
-                four(m, x);
-                four(v, y);
-                store_f32<WHOLE>(pm, i, n, x);
-                store_f32<WHOLE>(pv, i, n, y);
-            } else {
-                const float mm = row_max(m), mv = row_max(v);
-                // one reciprocal for both: even lanes take one moment's, odd lanes the other's
-                const float most = lane & 1 ? mv : mm, per = __frcp_rn(most) * 448.f;
-                const float per_m = __shfl_sync(0xffffffffu, per, 0), per_v = __shfl_sync(0xffffffffu, per, 1);
-                uint32_t qm = 0, qv = 0;
-                float scale = most * (1.f / 448.f);
-                if (held(mm) && held(mv)) {
-                    qm = codes(m, per_m, bits);
-                    qv = codes_positive(v, per_v, bits);
-                } else {
-                    if (held(mm)) qm = codes(m, per_m, bits);
-                    if (held(mv)) qv = codes_positive(v, per_v, bits);
-                    // a row of next to nothing is zeros; one with an entry that is no number, or infinite, is no numbers throughout
-                    if (!held(most)) scale = most < kDead ? 0.f : __int_as_float(0x7fc00000);
-                }
-                store_b8<WHOLE>(pm, i, n, qm);
-                store_b8<WHOLE>(pv, i, n, qv);
-                if (lane < 2 && (WHOLE || i - lane * 4 < n)) (lane ? pvs : pms)[i / kRow] = scale;
+                store_f32<WHOLE>(pp, i + 4 * f, n, x);
+                h[2 * f] = two_bf16(x[0], x[1]);
+                h[2 * f + 1] = two_bf16(x[2], x[3]);
             }
         }
-    };
-    auto advance = [&](int chunks) {
-        pg += chunks * kChunk * kG;
-        pp += chunks * kChunk * kP;
-        pm += chunks * kChunk * kS;
-        pv += chunks * kChunk * kS;
-        if (pc) pc += chunks * kChunk * 2;
-        if (Q8) { pms += chunks * (kChunk / kRow); pvs += chunks * (kChunk / kRow); }
-        row0 += chunks * (kChunk / kRow);
+        char* low = PB ? pp : pc;
+        if (PB || low) {
+            if (WHOLE) *reinterpret_cast<uint4*>(low + i * 2) = make_uint4(h[0], h[1], h[2], h[3]);
+            else { store_bf16<false>(low, 0, n, h[0], h[1]); store_bf16<false>(low, 4, n, h[2], h[3]); }
+        }
+        // the largest entries of the row: half of its lanes go on with the first moment, half with the second
+        const float lm = most_of(m), lv = most_of(v);
+        uint32_t bits_of = max(__float_as_uint(second ? lv : lm), __shfl_xor_sync(0xffffffffu, __float_as_uint(second ? lm : lv), 8));      // (bits of non-negative floats are ordered like them)
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) bits_of = max(bits_of, __shfl_xor_sync(0xffffffffu, bits_of, o));
+        const float most = __uint_as_float(bits_of), per = __frcp_rn(most) * 448.f, other = __shfl_xor_sync(0xffffffffu, per, 8);
+        const float per_m = second ? other : per, per_v = second ? per : other;
+        float scale = most * (1.f / 448.f);
+        uint2 qm = make_uint2(codes(m[0], per_m, bits), codes(m[1], per_m, bits + 4)), qv = make_uint2(codes_positive(v[0], per_v, bits), codes_positive(v[1], per_v, bits + 4));
+        if (!__all_sync(0xffffffffu, held(most))) {
+            // a row of next to nothing is zeros; one with an entry that is no number, or infinite, is no numbers throughout
+            const bool mine = held(most), its = __shfl_xor_sync(0xffffffffu, (int)mine, 8);
+            if (!(second ? its : mine)) qm = make_uint2(0, 0);
+            if (!(second ? mine : its)) qv = make_uint2(0, 0);
+            if (!mine) scale = most < kDead ? 0.f : __int_as_float(0x7fc00000);
+        }
+        if (WHOLE) {
+            *reinterpret_cast<uint2*>(pm + i) = qm;
+            *reinterpret_cast<uint2*>(pv + i) = qv;
+        } else {
+            store_b8<false>(pm, 0, n, qm.x);
+            store_b8<false>(pm, 4, n, qm.y);
+            store_b8<false>(pv, 0, n, qv.x);
+            store_b8<false>(pv, 4, n, qv.y);
+        }
+        if ((lane & 7) == 0 && (WHOLE || n + (second ? 8 * kWide : 0) > 0)) (second ? pvs : pms)[i / kRow] = scale;      // (n counts from this lane's first element)
     };
     Raw x;
-    if (Q8 && WHOLE) {      // the next chunk is on its way during the arithmetic of this one, which takes as long as its bytes
+    if (WHOLE) {      // the next chunk is on its way during the arithmetic of this one, which takes as long as its bytes
         Raw y;
         load(x, 0);
         for (; count > 0; count -= 2) {
@@ -484,14 +551,18 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
                 if (count > 2) load(x, 2);
                 compute(y, 1);
             }
-            advance(2);
+            pg += 2 * kChunk * kG;
+            pp += 2 * kChunk * kP;
+            pm += 2 * kChunk;
+            pv += 2 * kChunk;
+            if (pc) pc += 2 * kChunk * 2;
+            pms += 2 * kChunk / kRow;
+            pvs += 2 * kChunk / kRow;
+            row += 2 * kChunk / kRow;
         }
     } else {
-        for (; count > 0; --count) {
-            load(x, 0);
-            compute(x, 0);
-            advance(1);
-        }
+        load(x, 0);
+        compute(x, 0);
     }
 }
 
@@ -524,9 +595,14 @@ __global__ void __launch_bounds__(kThreads, kBlocks<Q8>) step_kernel(const __gri
     for (uint32_t c = blockIdx.x; c < a.units; c += gridDim.x) {
         at = tensor_of(a, c, at);
         const Tensor& t = a.t[at];
-        const Share s(t, c, a.span, warp, lane);
-        if (s.whole) update<Q8, PB, GB, true>(t, k, s.begin, s.own, s.whole, 0, lane);
-        if (s.rest) update<Q8, PB, GB, false>(t, k, s.begin + s.whole * kChunk, s.own, 1, s.rest, lane);
+        const Share s(t, c, a.span);
+        if (Q8) {
+            if (s.whole) update_q8<PB, GB, true>(t, k, s.begin, s.whole, 0, warp, lane);
+            if (s.rest) update_q8<PB, GB, false>(t, k, s.begin + s.whole * kChunk, 1, s.rest, warp, lane);
+        } else {
+            if (s.whole) update<PB, GB, true>(t, k, s.begin, s.whole, 0, warp, lane);
+            if (s.rest) update<PB, GB, false>(t, k, s.begin + s.whole * kChunk, 1, s.rest, warp, lane);
+        }
     }
 }
 
