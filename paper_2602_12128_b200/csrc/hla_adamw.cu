@@ -3,11 +3,11 @@
 //     m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2,   p' = p - lr wd p - lr / (1 - b1^t) m' / (sqrt(v' / (1 - b2^t)) + eps)
 //
 // What bounds it: with fp32 moments memory (28 bytes an element with fp32 weights, their bf16 copies and bf16 gradients: 227 M elements in
-// 1063 us, 5.98 TB/s, and 85 us for the norm's pass over the gradients).  With 8-bit moments and bf16 weights (10 bytes) the arithmetic: 62
-// instructions an element, a third of them integer ones, 564 us at 72 % of the issue slots, where the bytes would take 353.
+// 1063 us, 5.98 TB/s, and 85 us for the norm's pass over the gradients).  With 8-bit moments and bf16 weights (10 bytes) the arithmetic: 54
+// instructions an element, 21 of them on the integer pipe, which takes one every other cycle: 490 us, where the bytes would take 353.
 //
-// Layout: a warp takes rows of 128 consecutive elements of a tensor, four per lane, so that every load of a row is contiguous whatever
-// the type (16 bytes a lane in fp32, 8 in bf16, 4 in 8 bits) and a row is also what shares a scale.  Tensors from a few weights to
+// Layout: a row is 128 consecutive elements of a tensor, which is also what shares a scale.  A warp takes two rows, four elements of each a lane (with
+// fp32 moments, so that every load is contiguous) or eight of one (8-bit moments).  Tensors from a few weights to
 // millions are cut into chunks of 16 rows; a launch knows up to kMany tensors of one type from its parameters alone (nothing to upload, a
 // captured step holds it) and its blocks go through the chunks in turns.
 //
@@ -36,8 +36,8 @@ constexpr int kRow = 128;                        // elements of a row: a scale o
 constexpr int kRows = 2;                         // rows of a warp per chunk
 constexpr int kChunk = kWarps * kRows * kRow;
 constexpr int kFew = 40, kMany = 360;            // tensors per launch: 3.7 and 32 KB of parameters
-// Blocks of a step on an SM.  8-bit states live on their arithmetic: three blocks with the registers for two rows side by side and the next two
-// on their way take 659 us over eight transformer blocks, four 687, two 704; one row at a time and five blocks 823.
+// Blocks of a step on an SM.  8-bit states live on their arithmetic: three blocks, with registers for the next chunk on its way, take 587 us (the norm
+// included) over eight transformer blocks, four 645, two 609; without the next chunk three take 673, four 632, five 638.
 template <bool Q8> constexpr int kBlocks = Q8 ? 3 : 4;
 constexpr float kDead = 7.888609052210118e-31f;  // 2^-100: a row whose largest entry is below is held as zeros (its scale could not be inverted)
 
@@ -435,7 +435,7 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
 }
 
 // 8-bit moments, the same chunks.  Half a warp has a row, eight elements a lane: what is done once a row and lane (maximum, reciprocal, key of
-// the random numbers, addresses) is done for twice as many elements.
+// the random numbers, addresses) is done for twice as many elements: 62 -> 54 instructions an element, 659 -> 587 us.
 template <bool PB, bool GB, bool WHOLE>
 __device__ __forceinline__ void update_q8(const Tensor& t, const Coefficients& k, long long begin, int count, int n, int warp, int lane) {
     constexpr int kP = PB ? 2 : 4, kG = GB ? 2 : 4, kWide = 8;
