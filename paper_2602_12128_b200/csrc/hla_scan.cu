@@ -226,6 +226,7 @@ constexpr int kMapsThere = 1, kStatesThere = 2;
 
 // The last warp of a block: a channel per lane.  It composes the maps of the block's warps, hands the result to the blocks of the cluster and,
 // from theirs, finds the state before each warp's tokens.  (Done by every thread for itself, this was five instructions of 34 an element.)
+// The other warps wait for it, so that what it reads it reads at once, ahead of the chain of products: 1 % of the whole.
 //
 // Every map of a piece is written by its block straight into the shared memory of all blocks of the cluster and counted by their barriers.
 // A buffer is written again two pieces later: by then its writer has had this block's map of the piece between, which this block sends
@@ -236,34 +237,51 @@ __device__ __forceinline__ float2 exchange(Exchange& e, int pieces, int rank, in
     float* before = &e.before[0][0].x + lane;
     float product = 1.f;      // of all factors: (product, carry) is the map of all pieces
     bool lost = false;
+    uint32_t there[kMaxCluster], bars[kMaxCluster];      // where this block's maps go in every block, and their barriers
+#pragma unroll
+    for (int i = 0; i < kMaxCluster; ++i) {
+        const int to = i < blocks ? i : 0;
+        there[i] = of_block(tc::smem_u32(&e.blocks[0][rank][lane]), to);
+        bars[i] = of_block(tc::smem_u32(&e.full[0]), to);
+    }
     for (int s = 0; s < pieces; ++s) {
         const int buffer = s & 1;
         if (lane == 0) tc::mbar_arrive_expect_tx(&e.full[buffer], blocks * kTile * (int)sizeof(float2));
         wait_at(kMapsThere);
-        float PA[kRuns / 2], PH[kRuns / 2], A = 1.f, H = 0.f;
+        float a[kRuns / 2], h[kRuns / 2], PA[kRuns / 2], PH[kRuns / 2], A = 1.f, H = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRuns / 2; ++w) {
+            a[w] = wa[w * kTile];
+            h[w] = wh[w * kTile];
+        }
 #pragma unroll
         for (int w = 0; w < kRuns / 2; ++w) {
             PA[w] = A;
             PH[w] = H;
-            const float a = wa[w * kTile], h = wh[w * kTile];
-            H = fmaf(a, H, h);
-            A *= a;
+            H = fmaf(a[w], H, h[w]);
+            A *= a[w];
         }
-        const uint32_t to = tc::smem_u32(&e.blocks[buffer][rank][lane]), bar = tc::smem_u32(&e.full[buffer]);
-        for (int i = 0; i < blocks; ++i)
-            asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(of_block(to, i)), "f"(A), "f"(H), "r"(of_block(bar, i)) : "memory");
+#pragma unroll
+        for (int i = 0; i < kMaxCluster; ++i)
+            if (i < blocks)
+                asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(there[i] + buffer * (uint32_t)sizeof(e.blocks[0])), "f"(A), "f"(H),
+                             "r"(bars[i] + buffer * (uint32_t)sizeof(uint64_t))
+                             : "memory");
         if (!lost && !tc::mbar_wait(&e.full[buffer], (s >> 1) & 1)) {      // (two seconds: the outputs from here on are not numbers)
             lost = true;
             carry = __int_as_float(0x7fc00000);
         }
+        float2 q[kMaxCluster];
+#pragma unroll
+        for (int i = 0; i < kMaxCluster; ++i) q[i] = e.blocks[buffer][i][lane];      // (those behind the last block's are not used)
         float mine = carry;
 #pragma unroll
         for (int i = 0; i < kMaxCluster; ++i) {
-            if (i >= blocks) break;
             if (i == rank) mine = carry;
-            const float2 q = e.blocks[buffer][i][lane];
-            carry = fmaf(q.x, carry, q.y);
-            product *= q.x;
+            if (i < blocks) {
+                carry = fmaf(q[i].x, carry, q[i].y);
+                product *= q[i].x;
+            }
         }
 #pragma unroll
         for (int w = 0; w < kRuns / 2; ++w) before[w * kTile] = fmaf(PA[w], mine, PH[w]);
