@@ -410,7 +410,7 @@ typedef struct {
     int32_t param_dtype, grad_dtype; /* hla_dtype                                                      */
 } hla_adamw_tensor;
 typedef struct {
-    double beta1, beta2, eps;    /* 0 <= beta < 1, eps > 0 (HLA_STATE_Q8: eps >= 2^-50)                */
+    double beta1, beta2, eps;    /* 0 <= beta < 1, eps >= 2^-126 (HLA_STATE_Q8: 2^-50)                    */
     int32_t state;               /* hla_state_type                                                     */
     uint64_t seed;
 } hla_adamw_config;

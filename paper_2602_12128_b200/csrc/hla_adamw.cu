@@ -186,13 +186,16 @@ __device__ __forceinline__ float max_abs(float a, float b, float c) {      // a 
     return r;
 }
 
+// Roots of second moments.  SMALL: of those below the smallest normal number too, which a tiny eps does not cover.
+template <bool SMALL>
 __device__ __forceinline__ float sqrt_fast(float x) {
     float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    if (SMALL) asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    else asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 
-__device__ __forceinline__ float reciprocal(float x) {
+__device__ __forceinline__ float reciprocal(float x) {      // (what is inverted is at least eps, which is a normal number)
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
@@ -337,12 +340,13 @@ struct Coefficients {
 
 // The new moments and weights of two elements.  The moments are formed in single products and sums, each rounded: what is rounded at random
 // to 8 bits is then the same in every program that follows the formula, and so are the codes.
+template <bool SMALL>
 __device__ __forceinline__ void advance2(const Coefficients& k, float size, float shrink, P2 g, P2& m, P2& v, P2& w) {
     g = mul2(g, twice(k.gain));
     m = sum2(mul2(twice(k.b1), m), mul2(twice(k.r1), g));
     v = sum2(mul2(twice(k.b2), v), mul2(mul2(twice(k.r2), g), g));
     const float2 square = both(v);
-    const float2 below = both(fma2(pair(sqrt_fast(square.x), sqrt_fast(square.y)), twice(k.inv2), twice(k.eps)));
+    const float2 below = both(fma2(pair(sqrt_fast<SMALL>(square.x), sqrt_fast<SMALL>(square.y)), twice(k.inv2), twice(k.eps)));
     w = fma2(twice(-size), mul2(m, pair(reciprocal(below.x), reciprocal(below.y))), fma2(twice(-shrink), w, w));
 }
 
@@ -408,7 +412,7 @@ __device__ __forceinline__ void update(const Tensor& t, const Coefficients& k, l
             unpack<false>(rm[r], m);
             unpack<false>(rv[r], v);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) advance2(k, size, shrink, g[j], m[j], v[j], w[j]);
+            for (int j = 0; j < 2; ++j) advance2<true>(k, size, shrink, g[j], m[j], v[j], w[j]);
             float x[4];
             four(w, x);
             if (PB) {
@@ -489,7 +493,7 @@ __device__ __forceinline__ void update_q8(const Tensor& t, const Coefficients& k
             for (int j = 0; j < 2; ++j) {
                 m[f][j] = mul2(decode2(cm[f] >> (16 * j)), twice(raw.sm));
                 v[f][j] = mul2(decode2(cv[f] >> (16 * j)), twice(raw.sv));
-                advance2(k, size, shrink, g[f][j], m[f][j], v[f][j], w[f][j]);
+                advance2<false>(k, size, shrink, g[f][j], m[f][j], v[f][j], w[f][j]);
             }
         uint32_t bits[8];
         random_words<4>(key, row + ahead * (kChunk / kRow), (lane & 15) * 4, bits);
@@ -751,7 +755,7 @@ extern "C" {
 hla_status hla_adamw_create(const hla_adamw_config* cfg, const hla_adamw_tensor* tensors, int32_t n, hla_adamw** out) {
     if (out) *out = nullptr;
     if (!cfg || !out || !tensors || n <= 0) return HLA_ERR_INVALID_ARG;
-    if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !(cfg->eps > 0.0) || !((float)cfg->eps > 0.f) || !isfinite(cfg->eps))
+    if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !(cfg->eps >= 0x1p-126) || !isfinite((float)cfg->eps))
         return HLA_ERR_INVALID_ARG;
     if (cfg->state != HLA_STATE_F32 && cfg->state != HLA_STATE_Q8) return HLA_ERR_INVALID_ARG;
     const bool q8 = cfg->state == HLA_STATE_Q8;

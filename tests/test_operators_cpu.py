@@ -137,6 +137,7 @@ def tensor(at=P, n=100, **kw):
     ([tensor(), tensor(P + (1 << 20), m=P + 384)], {}, INVALID),                           # a moment over the end of another's weights
     ([tensor(grad=P + 16)], {}, INVALID),                                                  # a gradient over its weights
     ([tensor(n=1 << 39)], {}, UNSUPPORTED),
+    ([tensor()], dict(eps=1e-40), INVALID), ([tensor()], dict(eps=2.0 ** -126), OK), ([tensor()], dict(eps=1e39), INVALID),      # eps as fp32 is a normal number
 ])
 def test_adamw_create(rows, kw, want):
     st, ctx = adamw(rows, **kw)
