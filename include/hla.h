@@ -388,7 +388,7 @@ hla_status hla_heads_destroy(hla_heads *ctx);
  *     g = grad_scale * min(1, max_norm / (norm + 1e-6)) * grad,      norm = |grad_scale| * || all grads ||_2     (max_norm > 0)
  *     m = beta1 m + (1 - beta1) g,    v = beta2 v + (1 - beta2) g^2
  *     param = param - rate * weight_decay * param - rate * (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),  rate = lr * lr_mul
- * With max_norm > 0 a step whose norm is not finite changes no tensor.
+ * With max_norm > 0 a step whose norm is not finite changes no tensor; nor does one whose number, read on the device, is below 1.
  * Weights are fp32 or bf16, gradients fp32 or bf16, tensor by tensor.  fp32 weights may have a bf16 `copy`, rounded to nearest, for
  * the kernels that read them; bf16 weights are rounded up or down at random with the probability that keeps the mean.
  * HLA_STATE_F32: m, v fp32.  HLA_STATE_Q8: m, v are e4m3 codes (1 byte an element) with an fp32 scale for every 128

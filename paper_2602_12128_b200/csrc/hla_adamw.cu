@@ -589,6 +589,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks<Q8>) step_kernel(const __gri
         if (!isfinite(norm)) return;      // nothing changes
         k.gain *= fminf(a.max_norm / (norm + 1e-6f), 1.f);
     }
+    if (step < 1) return;      // (the host refuses such a step where it knows it)
     __syncthreads();
     k.b1 = a.b1; k.r1 = a.r1; k.b2 = a.b2; k.r2 = a.r2; k.eps = a.eps;
     k.lr = a.lr_device ? *a.lr_device : a.lr;
@@ -829,6 +830,8 @@ hla_status hla_adamw_step(hla_adamw* c, const hla_adamw_step_args* s, void* work
     if (!s->step_device && s->step < 1) return HLA_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(s->step_device) & 7u) || (reinterpret_cast<uintptr_t>(s->lr_device) & 3u) || (reinterpret_cast<uintptr_t>(s->norm) & 3u))
         return HLA_ERR_INVALID_ARG;
+    // blocks read the two scalars while one writes the norm
+    if (s->max_norm > 0.f && s->norm && ((s->lr_device && overlap(s->norm, 4, s->lr_device, 4)) || (s->step_device && overlap(s->norm, 4, s->step_device, 8)))) return HLA_ERR_INVALID_ARG;
     if (c->t.empty())      // nothing but a norm of nothing
         return s->max_norm > 0.f && s->norm && cudaMemsetAsync(s->norm, 0, 4, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess ? HLA_ERR_CUDA : HLA_OK;
     if (s->max_norm > 0.f) {

@@ -185,6 +185,18 @@ def test_second_moments_below_the_normal_numbers_with_an_eps_that_does_not_cover
     assert ((p.double() - want).abs() <= slack).all()
 
 
+@pytest.mark.parametrize("state", ["f32", "q8"])
+def test_a_step_below_one_on_the_device_changes_nothing(state):
+    g, p = torch.randn(300, device="cuda"), torch.randn(300, device="cuda")
+    before = p.clone()
+    opt = binding.AdamW([p], [g], state=state)
+    for number in (0, -5):
+        opt.step(1e-3, step=torch.tensor(number, device="cuda"), max_norm=1.0)
+        assert torch.equal(p, before) and not opt.ms[0].any() and not opt.vs[0].any()
+    opt.step(1e-3, step=torch.tensor(1, device="cuda"), max_norm=1.0)
+    assert not torch.equal(p, before) and torch.isfinite(p).all()
+
+
 def test_codes_are_those_of_the_formula():
     """Three steps of 8-bit states on several tensors: every code and scale is what moments formed in single rounded products and sums and the random
     numbers of (seed, step, tensor, element) give, so that another program can follow.  (Below the normal codes a value is first rounded to 2^-20 of

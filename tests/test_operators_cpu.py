@@ -169,6 +169,18 @@ def test_adamw_calls_are_checked_before_launching():
     assert lib.hla_adamw_destroy(None) == INVALID
 
 
+def test_the_norm_of_a_step_is_not_written_over_what_the_step_reads():
+    lib = b.load_library()
+    st, ctx = adamw([tensor()])
+    assert st == OK
+    need = lib.hla_adamw_workspace_bytes(ctx)
+    at = P + (1 << 22)
+    for kw in (dict(lr_device=at, norm=at), dict(step_device=at, norm=at + 4)):
+        a = b.HlaAdamwStepArgs(1e-3, 1, kw.get("lr_device", 0), kw.get("step_device", 0), 1.0, 1.0, kw["norm"])
+        assert lib.hla_adamw_step(ctx, ctypes.byref(a), P + (1 << 23), need, None) == INVALID
+    lib.hla_adamw_destroy(ctx)
+
+
 def test_adamw_binding_refuses():
     p = [torch.zeros(10)]
     for bad in (dict(params=p, grads=[torch.zeros(10)]), dict(params=p, grads=[]), dict(params=[torch.zeros(10, dtype=torch.float64)], grads=p),
