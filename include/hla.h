@@ -350,7 +350,8 @@ typedef struct {
 } hla_heads_config;
 
 /* A tensor [B][N][H][d] whose rows of H*d elements are contiguous: strides in elements, in whole 16-byte pieces (a
- * projection [B][N][3][H][d] has token stride 3*H*d). */
+ * projection [B][N][3][H][d] has token stride 3*H*d).  Rows do not share memory: either batches lie one behind another, or
+ * every token's batches behind those of the token before ([N][B][H][d]). */
 typedef struct {
     const void *data;
     int64_t batch_stride, token_stride;
@@ -371,10 +372,11 @@ hla_status hla_heads_forward(hla_heads *ctx, const hla_rows *q, const hla_rows *
                              const int32_t *positions, int64_t positions_batch_stride, void *Q, void *K, void *V, void *cuda_stream);
 
 /*
- * Gradients of sum(dQ Q + dK K + dV V): dq, dk, dv with strides of their own (so that they can be parts of one tensor that the
- * projection's backward reads), and dwq, dwk (fp32 [d], overwritten; NULL: not wanted).  dQ, dK, dV may be NULL together with
- * their outputs.  q and k are only read with norm = 1 and are the inputs of the forward.  The sums of dwq and dwk are formed
- * in a fixed order.  dV alone moves a head-major tensor [B][H][N][d] to token-major rows, as an output projection reads them.
+ * Gradients of sum(dQ Q + dK K + dV V): dq, dk, dv with strides of their own, and dwq, dwk (fp32 [d], overwritten; NULL: not wanted).
+ * dq, dk, dv can be parts of one tensor that the projection's backward reads: of equal strides then, the larger a multiple of the
+ * smaller.  dQ, dK, dV may be NULL together with their outputs.  q and k are only read with norm = 1 and are the inputs of the
+ * forward.  The sums of dwq and dwk are formed in a fixed order.  dV alone moves a head-major tensor [B][H][N][d] to token-major rows,
+ * as an output projection reads them.
  */
 hla_status hla_heads_backward(hla_heads *ctx, const void *dQ, const void *dK, const void *dV, const hla_rows *q, const hla_rows *k,
                               const void *wq, const void *wk, const int32_t *positions, int64_t positions_batch_stride,

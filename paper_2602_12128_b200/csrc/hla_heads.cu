@@ -499,13 +499,30 @@ bool rows_ok(const hla_heads* c, const hla_rows* r) {
     const bool tokens = c->cfg.N > 1, batches = c->cfg.B > 1;      // a stride of one step is never taken
     constexpr long long most = 1ll << 56;      // (spans are computed in 64 bits)
     if (tokens && (r->token_stride < width || r->token_stride > most / c->cfg.N || (r->token_stride * elt & 15))) return false;
-    if (batches && (r->batch_stride < (tokens ? (c->cfg.N - 1) * r->token_stride : 0) + width || r->batch_stride > most / c->cfg.B || (r->batch_stride * elt & 15))) return false;
+    if (batches && (r->batch_stride < width || r->batch_stride > most / c->cfg.B || (r->batch_stride * elt & 15))) return false;
+    // rows do not share memory: a batch lies behind the one before, or a token's batches behind those of the token before
+    if (tokens && batches && r->batch_stride < (c->cfg.N - 1) * r->token_stride + width && r->token_stride < (c->cfg.B - 1) * r->batch_stride + width) return false;
     return true;
 }
 
 size_t rows_span(const hla_heads* c, const hla_rows* r) {
     return (size_t)((c->cfg.B > 1 ? (c->cfg.B - 1) * r->batch_stride : 0) + (c->cfg.N > 1 ? (c->cfg.N - 1) * r->token_stride : 0) + (long long)c->cfg.H * c->cfg.d) *
            elt_size(c->cfg.dtype);
+}
+
+// Whether rows of a and rows of b, both written, may share memory.  Parts of one tensor do not: their strides are the same, the larger one a
+// multiple of the smaller, and within the smaller one they lie side by side.
+bool outputs_clash(const hla_heads* c, const hla_rows_out* a, const hla_rows_out* b) {
+    const hla_rows x = {a->data, a->batch_stride, a->token_stride}, y = {b->data, b->batch_stride, b->token_stride};
+    if (!overlap(x.data, rows_span(c, &x), y.data, rows_span(c, &y))) return false;
+    const bool tokens = c->cfg.N > 1, batches = c->cfg.B > 1;
+    if ((tokens && x.token_stride != y.token_stride) || (batches && x.batch_stride != y.batch_stride)) return true;
+    const long long t = tokens ? x.token_stride : x.batch_stride, n = batches ? x.batch_stride : t;      // (with one row each, overlapping spans are the rows)
+    const long long step = t < n ? t : n, elt = elt_size(c->cfg.dtype), width = (long long)c->cfg.H * c->cfg.d;
+    if ((!tokens && !batches) || (t < n ? n : t) % step) return true;
+    const uintptr_t from = reinterpret_cast<uintptr_t>(x.data), to = reinterpret_cast<uintptr_t>(y.data);
+    const long long off = (long long)((from < to ? to - from : from - to) % (unsigned long long)(step * elt));
+    return off < width * elt || step * elt - off < width * elt;
 }
 
 heads::Args common_args(const hla_heads* c, const int32_t* positions, int64_t pos_batch) {
@@ -609,6 +626,11 @@ hla_status hla_heads_create(const hla_heads_config* cfg, hla_heads** out) {
             x->turns[pair] = (c.inv_freq ? c.inv_freq[pair] : pow(x->cfg.theta, -(double)j / np)) / 6.283185307179586476925287;
         x->pair_end[i] = pair;
     }
+    for (int p = 0; p < rot / 2; ++p)
+        if (!isfinite(x->turns[p] * 0x1p31)) {      // (the farthest position; a product that is not finite has no fraction)
+            delete x;
+            return HLA_ERR_INVALID_ARG;
+        }
     x->log_lanes = 0;
     while ((per << x->log_lanes) < c.d) ++x->log_lanes;
     x->sm_count = current_sm_count();
@@ -688,6 +710,8 @@ hla_status hla_heads_backward(hla_heads* c, const void* dQ, const void* dK, cons
         const hla_rows o = {to[i]->data, to[i]->batch_stride, to[i]->token_stride};
         if (!aligned16(dy[i]) || !rows_ok(c, &o)) return HLA_ERR_INVALID_ARG;
         if (needs_x && (!x[i] || !rows_ok(c, x[i]))) return HLA_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (dy[j] && outputs_clash(c, to[i], to[j])) return HLA_ERR_INVALID_ARG;
         for (int j = 0; j < 3; ++j) {
             if (dy[j] && overlap(o.data, rows_span(c, &o), dy[j], dense)) return HLA_ERR_INVALID_ARG;
             if (j < 2 && c->cfg.norm && x[j] && x[j]->data && dy[j] && overlap(o.data, rows_span(c, &o), x[j]->data, rows_span(c, x[j]))) return HLA_ERR_INVALID_ARG;
@@ -708,6 +732,8 @@ hla_status hla_heads_backward(hla_heads* c, const void* dQ, const void* dK, cons
         t.rotate = i < 2;
     }
     a.want_dw = sums[0] || sums[1];
+    const size_t weights = (size_t)c->cfg.d * sizeof(float);
+    if (dwq && dwk && overlap(dwq, weights, dwk, weights)) return HLA_ERR_INVALID_ARG;
     if (a.want_dw) {
         if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
         if (workspace_bytes < hla_heads_workspace_bytes(c)) return HLA_ERR_WORKSPACE;

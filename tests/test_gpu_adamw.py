@@ -172,7 +172,7 @@ def test_gradients_of_any_size(size):
 
 
 def test_second_moments_below_the_normal_numbers_with_an_eps_that_does_not_cover_them():
-    """The first step moves a weight by lr g / (|g| + eps) whatever the size of g.  Second moments from 1e-39 on are held in multiples of 2^-149;
+    """The first step moves a weight by -lr g / (|g| + eps) whatever the size of g.  Second moments from 1e-39 on are held in multiples of 2^-149;
     two products round to them, half a multiple each, and a root halves the relative error."""
     g = (1 + 9 * torch.rand(1000, device="cuda")) * 1e-18
     g[::2] *= -1
@@ -180,7 +180,7 @@ def test_second_moments_below_the_normal_numbers_with_an_eps_that_does_not_cover
     p = torch.zeros(1000, device="cuda")
     opt = binding.AdamW([p], [g], eps=2.0 ** -126)
     opt.step(1e-3)
-    want = 1e-3 * g.double().sign()
+    want = -1e-3 * g.double().sign()
     slack = (32 * U + 2.0 ** -149 / (2 * 1e-3 * g.double().square()).clamp_min(1e-45)) * want.abs()
     assert ((p.double() - want).abs() <= slack).all()
 

@@ -166,6 +166,20 @@ def test_gradients_go_into_one_projection_and_nothing_else_is_written():
     assert (buf[keep] == 7).all()
 
 
+@pytest.mark.parametrize("B,N", [(3, 30), (5, 1)])
+def test_tokens_outside_the_batches(B, N):
+    """[N][B][3][H][d]: the batches of a token lie behind one another, of inputs and gradients."""
+    H, d, grid = 3, 64, (1, 1, N)
+    op, xs, ws, ds = make(B, H, grid, d, "bf16", (24, 20, 20))
+    outside = lambda: torch.full((N, B + 1, 3, H, d), 7.0, device="cuda", dtype=torch.bfloat16)
+    X, dX = outside(), outside()
+    parts = lambda t: [t[:, :B, i].transpose(0, 1) for i in range(3)]
+    for to, x in zip(parts(X), xs):
+        to.copy_(x)
+    verify(op, parts(X), ws, ds, ref.angles(ref.grid_positions(grid), (24, 20, 20)), "interleaved", True, 1.0, "bf16", (24, 20, 20), dX=parts(dX))
+    assert (dX[:, B:] == 7).all()
+
+
 def test_each_tensor_alone():
     op, xs, ws, ds = make(2, 6, (2, 5, 3), 128, "bf16", (44, 42, 42))
     Q, K, V = op.forward(*xs, *ws)

@@ -90,6 +90,40 @@ def test_a_single_token_or_sequence_may_have_any_stride():
     lib.hla_heads_destroy(ctx)
 
 
+def test_heads_gradients_that_would_share_rows_are_refused():
+    lib = b.load_library()
+    st, ctx = heads(norm=0)
+    assert st == OK
+    row, far = 3 * 64, P + (1 << 24)                       # elements of a token's heads; two bytes each
+    r = lambda at, batch, token: ctypes.byref(b.HlaRows(at, batch, token))
+    bwd = lambda dq, dk: lib.hla_heads_backward(ctx, P, P, None, None, None, None, None, None, 0, dq, dk, None, None, None, None, 0, None)
+    fused = lambda part, token=3 * row, batch=24 * 3 * row: r(far + part * row * 2, batch, token)
+    assert bwd(fused(0), fused(0)) == INVALID                                            # the same rows twice
+    assert bwd(fused(0), r(far + row, 72 * row, 3 * row)) == INVALID                     # half of a row
+    assert bwd(fused(0), r(far + (3 * row - 8) * 2, 72 * row, 3 * row)) == INVALID       # the end over the next token's begin
+    assert bwd(fused(0), r(far + 3 * row * 2, 72 * row, 3 * row)) == INVALID             # one token on
+    assert bwd(fused(0), r(far + row * 2, 24 * row, row)) == INVALID                     # other strides
+    assert bwd(fused(0, batch=72 * row + 64), fused(1, batch=72 * row + 64)) == INVALID  # not a multiple
+    assert bwd(r(far, 3 * row, 6 * row), r(far + 3 * row * 2, 3 * row, 6 * row)) == INVALID      # [N][B][3]: one batch on
+    lib.hla_heads_destroy(ctx)
+    st, ctx = heads()
+    need = lib.hla_heads_workspace_bytes(ctx)
+    x = lambda at: r(at, 24 * row, row)
+    call = lambda dwq, dwk: lib.hla_heads_backward(ctx, P, P, None, x(2 * far), x(2 * far), None, None, None, 0, fused(0), fused(1), None, dwq, dwk, 3 * far & ~255, need, None)
+    assert call(4 * far, 4 * far) == INVALID and call(4 * far, 4 * far + 252) == INVALID
+    lib.hla_heads_destroy(ctx)
+
+
+def test_heads_frequencies_that_leave_64_bits():
+    for value, want in ((1e305, INVALID), (float("inf"), INVALID), (1e200, OK)):
+        f = (ctypes.c_double * 32)(*([1.0] * 31 + [value]))
+        st, ctx = heads(inv_freq=f)
+        assert st == want
+        if ctx:
+            b.load_library().hla_heads_destroy(ctx)
+    assert heads(d=128, n_axes=1, axis_width=(128, 0, 0), grid=(24, 0, 0), theta=1e-320)[0] == INVALID      # its last frequency is 1e315
+
+
 def test_heads_binding_refuses():
     with pytest.raises(ValueError):
         b.Heads(1, 2, 24, 64, dtype="f16", device=None)
