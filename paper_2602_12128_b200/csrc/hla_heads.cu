@@ -24,7 +24,7 @@ namespace heads {
 
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = kMaxD / 2;
-constexpr int kDwThreads = 1024;
+constexpr int kDwThreads = 1024, kDwChannels = 8;
 constexpr int kStages = 4;          // rows of a group on their way in the backward
 
 struct Tensor {
@@ -434,23 +434,30 @@ __global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_cons
     }
 }
 
-// Sums the partial rows of one tensor (blockIdx.y) for 32 channels (blockIdx.x) in a fixed order.
+// Sums the partial rows of one tensor (blockIdx.y) for kDwChannels channels (blockIdx.x: a sector of every row) in a fixed order: rows by the
+// block's slices, a warp's slices, warps.  What it takes is latency: all rows of a thread are on their way at once.
 __global__ void __launch_bounds__(kDwThreads) dw_kernel(const float* part, int rows, int d, float* dw0, float* dw1) {
-    __shared__ double sums[32][33];
-    const int ch = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
+    constexpr int kSlices = kDwThreads / kDwChannels, kWarps = kDwThreads / 32;
+    __shared__ double sums[kDwChannels][kWarps];
+    const int ch = blockIdx.x * kDwChannels + threadIdx.x % kDwChannels, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     wait_for_previous_kernel();
     const float* mine = part + (size_t)blockIdx.y * rows * d;
     double v = 0.0;
     if (ch < d) {
 #pragma unroll 8
-        for (int r = slice; r < rows; r += 32) v += mine[(size_t)r * d + ch];
+        for (int r = threadIdx.x / kDwChannels; r < rows; r += kSlices) v += mine[(size_t)r * d + ch];
     }
-    sums[slice][threadIdx.x & 31] = v;
+#pragma unroll
+    for (int o = 16; o >= kDwChannels; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (lane < kDwChannels) sums[lane][warp] = v;
     __syncthreads();
-    if (slice == 0 && ch < d) {
-        for (int i = 1; i < 32; ++i) v += sums[i][threadIdx.x];
+    if (warp < kDwChannels) {      // a channel a warp
+        static_assert(kWarps == 32, "a warp has the sums of all warps");
+        v = sums[warp][lane];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         float* dw = blockIdx.y ? dw1 : dw0;
-        if (dw) dw[ch] = (float)v;
+        if (dw && lane == 0 && blockIdx.x * kDwChannels + warp < d) dw[blockIdx.x * kDwChannels + warp] = (float)v;
     }
 }
 
@@ -746,7 +753,7 @@ hla_status hla_heads_backward(hla_heads* c, const void* dQ, const void* dK, cons
     const Kernel kern = pick<Bwd>(c);
     kern<<<dim3(blocks, a.n_tensors * a.chunks), heads::kThreads, 0, st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return HLA_ERR_CUDA;
-    if (a.want_dw && !launch_behind(heads::dw_kernel, dim3((a.d + 31) / 32, normed), heads::kDwThreads, st, (const float*)a.part, a.chunks * blocks, a.d, sums[0], sums[1]))
+    if (a.want_dw && !launch_behind(heads::dw_kernel, dim3((a.d + heads::kDwChannels - 1) / heads::kDwChannels, normed), heads::kDwThreads, st, (const float*)a.part, a.chunks * blocks, a.d, sums[0], sums[1]))
         return HLA_ERR_CUDA;
     return HLA_OK;
 }
