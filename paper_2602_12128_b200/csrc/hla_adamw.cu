@@ -3,7 +3,7 @@
 //     m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2,   p' = p - lr wd p - lr / (1 - b1^t) m' / (sqrt(v' / (1 - b2^t)) + eps)
 //
 // What bounds it: with fp32 moments memory (28 bytes an element with fp32 weights, their bf16 copies and bf16 gradients: 227 M elements in
-// 1063 us, 5.98 TB/s, and 85 us for the norm's pass over the gradients).  With 8-bit moments and bf16 weights (10 bytes) the arithmetic: 54
+// 1018 us, 6.24 TB/s, and 79 us for the norm's pass over the gradients).  With 8-bit moments and bf16 weights (10 bytes) the arithmetic: 54
 // instructions an element, 21 of them on the integer pipe, which takes one every other cycle: 490 us, where the bytes would take 353.
 //
 // Layout: a row is 128 consecutive elements of a tensor, which is also what shares a scale.  A warp takes two rows, four elements of each a lane (with
@@ -36,9 +36,12 @@ constexpr int kRow = 128;                        // elements of a row: a scale o
 constexpr int kRows = 2;                         // rows of a warp per chunk
 constexpr int kChunk = kWarps * kRows * kRow;
 constexpr int kFew = 40, kMany = 360;            // tensors per launch: 3.7 and 32 KB of parameters
-// Blocks of a step on an SM.  8-bit states live on their arithmetic: three blocks, with registers for the next chunk on its way, take 587 us (the norm
-// included) over eight transformer blocks, four 645, two 609; without the next chunk three take 673, four 632, five 638.
-template <bool Q8> constexpr int kBlocks = Q8 ? 3 : 4;
+// Blocks of a step on an SM, and the most chunks of a turn.  8-bit states live on their arithmetic: three blocks, with registers for the next chunk
+// on its way, take 587 us (the norm included) over eight transformer blocks, four 645, two 609; without the next chunk three take 673, four 632,
+// five 638.  fp32 moments live on memory, which likes few places at a time: one block 1239 us, two 1120, three 1143, four 1152, five 1166; two
+// with turns of one chunk 1175, two 1127, four 1108, eight 1116, sixteen 1123.  The next chunk in registers changes nothing there (1111).
+template <bool Q8> constexpr int kBlocks = Q8 ? 3 : 2;
+template <bool Q8> constexpr int kSpan = Q8 ? 8 : 4;
 constexpr float kDead = 7.888609052210118e-31f;  // 2^-100: a row whose largest entry is below is held as zeros (its scale could not be inverted)
 
 struct Tensor {
@@ -672,12 +675,13 @@ hla_status check_spans(const hla_adamw* c) {
 }
 
 // Chunks that a block takes in one turn.  Finding a tensor and its pointers costs about 80 instructions, ten an element of a chunk; where
-// every block has at least 16 turns, eight chunks share them.
+// every SM has at least 64 turns, up to kSpan chunks share them.
 int span(const hla_adamw* c, int from, int n) {
+    const int most = c->cfg.state == HLA_STATE_Q8 ? adamw::kSpan<true> : adamw::kSpan<false>;
     long long chunks = 0;
     for (int i = 0; i < n; ++i) chunks += (c->t[from + i].n + adamw::kChunk - 1) / adamw::kChunk;
     int s = 1;
-    while (s < 8 && chunks >= 2ll * s * 16 * adamw::kBlocks<false> * c->sm_count) s *= 2;
+    while (s < most && chunks >= 2ll * s * 64 * c->sm_count) s *= 2;
     return s;
 }
 
