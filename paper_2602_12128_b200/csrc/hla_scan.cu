@@ -19,6 +19,7 @@
 #include "../../include/hla.h"
 
 #include <new>
+#include <type_traits>
 
 #include "hla_ops_common.cuh"
 #include "hla_tc_prim.cuh"
@@ -483,36 +484,41 @@ __global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid
         cluster_sync();      // no block leaves while another may still write into its shared memory
         return;
     }
-    for (int s = 0, stage = 0; s < p.pieces; ++s) {
-        arrived<kStages - 1>();
+    // one piece; WHOLE: the warp's tokens and channels are all there, and the sequence's first token is not among them
+    auto piece = [&](auto whole_, int stage) {
+        constexpr bool WHOLE = decltype(whole_)::value;
         const uint32_t from = mine + stage * (kInputs * S::kBytes) + own;
-        const bool whole = live && i0 + kRun < p.N;
         P2 a[kRun], rest[kRun], A, M;
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
             gate<GATE>(V::get(read<Raw>(from + k * S::kRowBytes)), a[k], rest[k]);
-            if (!whole && i0 + k >= p.N) a[k] = twice(1.f);      // (its dh was not read and is zero)
+            if (!WHOLE && i0 + k >= p.N) a[k] = twice(1.f);      // (its dh was not read and is zero)
             const P2 dk = V::get(read<Raw>(from + S::kBytes + k * S::kRowBytes));
             M = mul2(a[k], k ? add2(dk, M) : dk);
             A = k ? mul2(a[k], A) : a[k];
         }
         P2 mu = state_before(e, A, M, warp, lane, late, [] {});
+        if (p.summary) return;
 #pragma unroll
         for (int k = 0; k < kRun; ++k) {
-            if (p.summary) break;
             const P2 lam = add2(V::get(read<Raw>(from + S::kBytes + k * S::kRowBytes)), mu);
             mu = mul2(a[k], lam);
             P2 w = V::get(read<Raw>(from + 2 * S::kBytes + k * S::kRowBytes));
-            if (!whole && i0 + k == p.N - 1) w = h0;
+            if (!WHOLE && i0 + k == p.N - 1) w = h0;
             if (CONVEX) w = fma2(V::get(read<Raw>(from + 3 * S::kBytes + k * S::kRowBytes)), twice(-1.f), w);
             P2 dg = mul2(mu, w);      // lambda a (h_{t-1} - x)
             if (GATE == kSigmoid) dg = mul2(dg, rest[k]);
             const P2 dx = CONVEX ? mul2(lam, rest[k]) : lam;
-            if (whole || (live && i0 + k < p.N)) {
-                V::template store<VEC>(po0 - k * os, second, dx);
-                V::template store<VEC>(po1 - k * os, second, dg);
+            if (WHOLE || (live && i0 + k < p.N)) {
+                V::template store<VEC>(po0 - k * os, WHOLE || second, dx);
+                V::template store<VEC>(po1 - k * os, WHOLE || second, dg);
             }
         }
+    };
+    for (int s = 0, stage = 0; s < p.pieces; ++s) {
+        arrived<kStages - 1>();
+        if (w0 + s * stride + 2 * kRun < p.N && channels >= kTile) piece(std::true_type{}, stage);
+        else piece(std::false_type{}, stage);
         __syncwarp();
         fetch(s + kStages, stage);
         stage ^= 1;
