@@ -13,9 +13,9 @@
 // through once more from the state that comes in; the next pieces are on their way into shared memory.  All orders are fixed: results
 // do not depend on timing.  States, maps and sums are fp32.
 //
-// Forward of 32760 tokens, 1536 channels, bf16, sigmoid gates, convex: 73 us, 4.1 TB/s of 6.5, 24.5 instructions an element, 54 % of the issue
+// Forward of 32760 tokens, 1536 channels, bf16, sigmoid gates, convex: 70 us, 4.3 TB/s of 6.5, 24.5 instructions an element, 54 % of the issue
 // slots.  The rest is the wait for the slowest block of a cluster (384 blocks on 148 SMs: three on some, two on others) and the round through the
-// cluster.  Backward of two such sequences, log gates: 213 us, 4.7 TB/s, 40 instructions an element at 67 %.
+// cluster.  Backward of two such sequences, log gates: 200 us, 5.0 TB/s, 32 instructions an element at 55 %.
 #include "../../include/hla.h"
 
 #include <new>
@@ -34,6 +34,11 @@ template <typename T> constexpr int kRunOf = sizeof(T) == 2 ? 8 : 4;            
 template <typename T> constexpr int kPieceOf = kRuns * kRunOf<T>;               // tokens of a block between two exchanges
 constexpr int kTile = 2 * kLanes;                // channels of a block
 constexpr int kMaxCluster = 8;
+constexpr int kBlocks = 3;                       // on an SM, and of the backward with many channels:
+// With three its time depends on where the clusters come to lie (2 x 32760 x 1536, log gates: 199 to 285 us, with two 197) and its registers do
+// not hold the tokens of a thread (convex, sigmoid gates: 297 us, with two 238).  Where clusters of eight fit at once three are better (32760 x
+// 1536, log gates: 94 us, with two 123).
+constexpr int kBlocksMany = 2;
 
 enum { kLog = 0, kSigmoid = 1 };
 
@@ -346,7 +351,7 @@ __device__ __forceinline__ void exchange_warp(Exchange& e, const Args& p, int ra
 }
 
 template <typename T, int GATE, bool CONVEX, int WIDE>
-__global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_constant__ Args p) {
+__global__ void __launch_bounds__(kThreads + 32, kBlocks) forward_kernel(const __grid_constant__ Args p) {
     using V = Two<T>;
     constexpr bool VEC = WIDE >= 2 * (int)sizeof(T);      // two channels of the outputs are one word
     using S = Stage<T>;
@@ -434,8 +439,8 @@ __global__ void __launch_bounds__(kThreads + 32, 3) forward_kernel(const __grid_
 }
 
 // Tokens are counted from the end: i = N - 1 - t; pointers go down.
-template <typename T, int GATE, bool CONVEX, int WIDE>
-__global__ void __launch_bounds__(kThreads + 32, 3) backward_kernel(const __grid_constant__ Args p) {
+template <typename T, int GATE, bool CONVEX, int WIDE, int BLOCKS>
+__global__ void __launch_bounds__(kThreads + 32, BLOCKS) backward_kernel(const __grid_constant__ Args p) {
     using V = Two<T>;
     constexpr bool VEC = WIDE >= 2 * (int)sizeof(T);      // two channels of the outputs are one word
     using Raw = typename V::Raw;
@@ -542,6 +547,7 @@ struct hla_scan {
     int sm_count;
     void (*ready[2])(scan::Args);      // forward and backward kernels that were given their shared memory, on `device`
     int device;
+    int blocks;                        // of a cluster of the backward
 };
 
 namespace {
@@ -560,7 +566,8 @@ Kernel pick(const hla_scan_config& c, int wide) {
     return wide == 16 ? pick_of<K, __nv_bfloat16, 16>(s, v) : wide == 4 ? pick_of<K, __nv_bfloat16, 4>(s, v) : pick_of<K, __nv_bfloat16, 2>(s, v);
 }
 template <typename T, int GATE, bool CONVEX, int WIDE> struct Fwd { static Kernel get() { return scan::forward_kernel<T, GATE, CONVEX, WIDE>; } };
-template <typename T, int GATE, bool CONVEX, int WIDE> struct Bwd { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX, WIDE>; } };
+template <typename T, int GATE, bool CONVEX, int WIDE> struct Bwd { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX, WIDE, scan::kBlocks>; } };
+template <typename T, int GATE, bool CONVEX, int WIDE> struct BwdMany { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX, WIDE, scan::kBlocksMany>; } };
 
 int elt_size(int dtype) { return dtype == HLA_BF16 ? 2 : 4; }
 
@@ -591,40 +598,84 @@ long long columns_of(const hla_scan* c) { return (long long)((c->cfg.C + scan::k
 // 64 channels 78 us in one part, 29 in 27; 512 channels backward 158 and 131 in three; 32760 tokens of 768 channels 49 and 70 in two, which
 // is not taken).
 int segments_of(const hla_scan* c, int blocks, long long pieces) {
-    long long n = 3ll * c->sm_count / (blocks * columns_of(c));
+    long long n = (long long)scan::kBlocks * c->sm_count / (blocks * columns_of(c));
     if (n > pieces / 2) n = pieces / 2;
     return n < 3 ? 1 : (int)n;
 }
 
+int piece_of(const hla_scan* c) { return c->cfg.dtype == HLA_BF16 ? scan::kPieceOf<__nv_bfloat16> : scan::kPieceOf<float>; }
+
+// Blocks of a cluster: as many as sequences and channels leave room for.  A second wave would wait for the first, and with fewer
+// blocks an exchange is shorter.  Forward of 32760 tokens of 1536 channels: two sequences 123 us with four blocks, 133 with eight; three 166 with
+// two, 192 with eight; four 231 with two, 252 with eight.  (Clusters do not fill the groups of SMs that they have to lie in: of eight blocks
+// 48 run at once on 148 SMs, of four 104.)
+int cluster_of(const hla_scan* c) {
+    const long long columns = columns_of(c), room = (long long)scan::kBlocks * c->sm_count;
+    auto fits = [&](int b) { return b * columns <= room - (b == 8 ? room / 8 : b == 4 ? room / 16 : 0); };
+    int blocks = 1;
+    while (blocks < scan::kMaxCluster && blocks * piece_of(c) < c->cfg.N && fits(2 * blocks)) blocks *= 2;
+    return blocks;
+}
+// The backward has many channels where longer clusters would have been of use and found no room.
+bool many(const hla_scan* c) {
+    const int blocks = cluster_of(c);
+    return blocks < scan::kMaxCluster && blocks * piece_of(c) < c->cfg.N;
+}
+// With many channels the backward's clusters are those with the least waves x tokens a block, the fewest blocks where it is the same.  Two sequences (three waves of clusters of
+// eight): 195 us, with four blocks (two waves) 200, with two (one) 225; three: 254 with two blocks, 307 with eight; four: 365 with four, 457 with two.
+bool backward_cluster(const hla_scan* c, Kernel kern, int bytes, int& blocks) {
+    long long best = 0;
+    for (int b = 1; b <= scan::kMaxCluster && (b == 1 || b / 2 * piece_of(c) < c->cfg.N); b *= 2) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(b);
+        cfg.blockDim = dim3(scan::kThreads + 32);
+        cfg.dynamicSmemBytes = bytes;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = b;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        int active = 0;
+        if (cudaOccupancyMaxActiveClusters(&active, kern, &cfg) != cudaSuccess || active <= 0) return false;
+        const long long cost = (columns_of(c) + active - 1) / active * (scan::kMaxCluster / b);
+        if (b == 1 || cost < best) {
+            best = cost;
+            blocks = b;
+        }
+    }
+    return true;
+}
+
 hla_status launch(hla_scan* c, bool back, Kernel kern, int bytes, scan::Args& a, void* workspace, size_t workspace_bytes, cudaStream_t st) {
-    int blocks = 1;      // of a cluster
-    const int piece = c->cfg.dtype == HLA_BF16 ? scan::kPieceOf<__nv_bfloat16> : scan::kPieceOf<float>;
-    // as many as sequences and channels leave room for (three blocks an SM): a second wave would wait for the first, and with fewer blocks in a
-    // cluster an exchange is shorter.  Backward of 2 x 32760 tokens, 1536 channels: 8 blocks a cluster (1.7 waves) 223 us, 4 blocks 213 us
-    const long long columns = columns_of(c), room = 3ll * c->sm_count;
-    while (blocks < scan::kMaxCluster && blocks * piece < a.N && 2 * blocks * columns <= room) blocks *= 2;
-    const long long total = ((long long)a.N + blocks * piece - 1) / (blocks * piece);
-    a.segments = segments_of(c, blocks, total);
-    a.pieces = (int)((total + a.segments - 1) / a.segments);
-    a.segments = (int)((total + a.pieces - 1) / a.pieces);
+    const bool choose = back && many(c);
+    const int piece = piece_of(c);
+    int blocks = cluster_of(c);
+    auto pieces = [&] { return ((long long)a.N + blocks * piece - 1) / (blocks * piece); };
+    a.segments = choose ? 1 : segments_of(c, blocks, pieces());
     a.maps = static_cast<float2*>(workspace);
     if (a.segments > 1) {
         if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
         if (workspace_bytes < hla_scan_workspace_bytes(c)) return HLA_ERR_WORKSPACE;
     }
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return HLA_ERR_CUDA;
+    if (c->ready[back] != kern || c->device != dev) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return HLA_ERR_CUDA;
+        if (choose && !backward_cluster(c, kern, bytes, c->blocks)) return HLA_ERR_CUDA;
+        if (c->device != dev) c->ready[!back] = nullptr;
+        c->ready[back] = kern;
+        c->device = dev;
+    }
+    if (choose) blocks = c->blocks;
+    const long long total = pieces();
+    a.pieces = (int)((total + a.segments - 1) / a.segments);
+    a.segments = (int)((total + a.pieces - 1) / a.pieces);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks, (a.C + scan::kTile - 1) / scan::kTile, c->cfg.B * a.segments);
     cfg.blockDim = dim3(scan::kThreads + 32);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return HLA_ERR_CUDA;
-    if (c->ready[back] != kern || c->device != dev) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return HLA_ERR_CUDA;
-        if (c->device != dev) c->ready[!back] = nullptr;
-        c->ready[back] = kern;
-        c->device = dev;
-    }
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = blocks;
@@ -727,7 +778,7 @@ hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const vo
     a.in = static_cast<const float*>(dh_last);
     a.h0 = static_cast<const float*>(h0);
     a.last = static_cast<float*>(dh0);
-    return launch(c, true, pick<Bwd>(c->cfg, width(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+    return launch(c, true, many(c) ? pick<BwdMany>(c->cfg, width(c, a)) : pick<Bwd>(c->cfg, width(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 hla_status hla_scan_destroy(hla_scan* c) {

@@ -100,6 +100,13 @@ def test_many_pieces(B, N, C, dtype, gate, convex):
     verify(B, N, C, dtype, gate, convex)
 
 
+@pytest.mark.parametrize("B,N,C,dtype,gate,convex", [(4, 700, 1540, "bf16", "log", False), (3, 300, 2001, "f32", "sigmoid", True), (2, 2100, 1536, "bf16", "sigmoid", True),
+                                                     (20, 140, 1000, "f32", "log", True), (2, 1025, 1601, "bf16", "log", True), (16, 1100, 1024, "bf16", "sigmoid", False)])
+def test_many_channels(B, N, C, dtype, gate, convex):
+    """More tiles of channels than clusters of eight blocks run at once."""
+    verify(B, N, C, dtype, gate, convex, fused=C == 1536, carry=C != 1024)
+
+
 @pytest.mark.parametrize("B,N,C,dtype,gate,convex", [(1, 20000, 33, "bf16", "log", True), (2, 9000, 64, "bf16", "sigmoid", True), (1, 8200, 1, "f32", "log", False),
                                                      (1, 16385, 257, "bf16", "log", False), (3, 6000, 20, "f32", "sigmoid", True)])
 @pytest.mark.parametrize("carry", [False, True])
