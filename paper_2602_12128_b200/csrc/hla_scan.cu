@@ -15,7 +15,7 @@
 //
 // Forward of 32760 tokens, 1536 channels, bf16, sigmoid gates, convex: 70 us, 4.3 TB/s of 6.5, 24.5 instructions an element, 54 % of the issue
 // slots.  The rest is the wait for the slowest block of a cluster (384 blocks on 148 SMs: three on some, two on others) and the round through the
-// cluster.  Backward of two such sequences, log gates: 200 us, 5.0 TB/s, 32 instructions an element at 55 %.
+// cluster.  Backward of two such sequences, log gates: 200 us, 5.0 TB/s, 30 instructions an element at 47 %.
 #include "../../include/hla.h"
 
 #include <new>
