@@ -56,7 +56,10 @@ struct Args {
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ uint32_t cluster_blocks() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+// The .aligned barriers want all lanes of a warp at once, and so do bar.sync and bar.arrive; lanes may come here apart (one of them has prepared
+// something, or a wait ended for one before the others), so each of them is behind a __syncwarp.
 __device__ __forceinline__ void cluster_sync() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -226,8 +229,8 @@ struct Exchange {
     uint64_t full[2];                                                   // barriers: the maps of all blocks are there
 };
 
-__device__ __forceinline__ void arrive_at(int barrier) { asm volatile("bar.arrive %0, %1;" ::"r"(barrier), "n"(kThreads + 32) : "memory"); }
-__device__ __forceinline__ void wait_at(int barrier) { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kThreads + 32) : "memory"); }
+__device__ __forceinline__ void arrive_at(int barrier) { __syncwarp(); asm volatile("bar.arrive %0, %1;" ::"r"(barrier), "n"(kThreads + 32) : "memory"); }
+__device__ __forceinline__ void wait_at(int barrier) { __syncwarp(); asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kThreads + 32) : "memory"); }
 constexpr int kMapsThere = 1, kStatesThere = 2;
 
 // The last warp of a block: a channel per lane.  It composes the maps of the block's warps, hands the result to the blocks of the cluster and,

@@ -1,0 +1,18 @@
+"""`bar.sync`, `bar.arrive` and the `.aligned` cluster barriers are undefined unless all lanes of a warp execute them together.  Where lanes may
+come apart before one (a lane that prepares something, a wait that ends for each lane by itself), a __syncwarp has to bring them together."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2602_12128_b200", "csrc")
+BARRIER = re.compile(r'asm volatile\("(bar\.(?:sync|arrive)|barrier\.cluster\.(?:arrive|wait)[^;"]*\.aligned)')
+
+
+def test_barriers_of_the_scan_are_reached_by_whole_warps():
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "hla_scan.cu")).read())
+    found = list(BARRIER.finditer(text))
+    assert len(found) == 4
+    for m in found:
+        body = text[text.rindex("{", 0, m.start()):m.start()]      # (of a function that is the barrier alone)
+        if "cluster.wait" in m.group(1):
+            assert "barrier.cluster.arrive" in body                 # directly behind the arrival
+        assert re.match(r"\{\s*__syncwarp\(\);", body), m.group(1)
