@@ -17,6 +17,7 @@
 #include <math.h>
 #include <new>
 
+#include "hla_heads_units.h"
 #include "hla_ops_common.cuh"
 
 namespace hla {
@@ -48,6 +49,7 @@ struct Args {
     int half;                    // offset of the second channel of a pair of the half-split pairing
     float eps, inv_d;
     int n_tensors, chunks, per_chunk;                // every tensor's heads in `chunks` runs of `per_chunk`
+    Units units;                 // forward
     Tensor t[3];
     float* part;                 // [tensor][chunk, block][d] partial sums of the weight gradients
     int want_dw;
@@ -202,16 +204,12 @@ __global__ void __launch_bounds__(kThreads, 4) forward_kernel(const __grid_const
     __syncthreads();
     const int log_lanes = LOG ? LOG : p.log_lanes;
     const int l = threadIdx.x & ((1 << log_lanes) - 1);
-    const uint32_t tokens = (uint32_t)p.B * p.N, units = tokens * p.n_tensors * p.chunks;
-    uint32_t unit = blockIdx.x * (uint32_t)(kThreads >> log_lanes) + (threadIdx.x >> log_lanes);
-    const bool live = unit < units;
-    if (!live) unit = 0;      // (stays for the shuffles of its warp)
-    const uint32_t run = unit / tokens, token = unit - run * tokens;
-    const int b = token / p.N, n = token - b * p.N;
-    const Tensor& t = p.t[run / p.chunks];
-    const int h0 = (run % p.chunks) * p.per_chunk, count = min(p.H - h0, p.per_chunk);
+    const Unit unit = unit_of(p.units, blockIdx.x * (uint32_t)(kThreads >> log_lanes) + (threadIdx.x >> log_lanes));      // (without work: stays for the shuffles of its warp)
+    const int b = unit.token / p.N, n = unit.token - b * p.N;
+    const Tensor& t = p.t[unit.run / p.chunks];
+    const int h0 = (unit.run % p.chunks) * p.per_chunk, count = min(p.H - h0, p.per_chunk);
     const Place<T, HALF> at(p, l);
-    const bool mine = live && at.in;
+    const bool mine = unit.live && at.in;
     const size_t row = (size_t)p.d * sizeof(T), head = row * p.N;
     const char* src = t.x + b * t.x_batch + n * t.x_token + h0 * row;
     char* dst = t.out + ((size_t)b * p.H + h0) * head + n * row;
@@ -686,10 +684,10 @@ hla_status hla_heads_forward(hla_heads* c, const hla_rows* q, const hla_rows* k,
     }
     a.per_chunk = heads_per_run(c, a.n_tensors);
     a.chunks = (a.H + a.per_chunk - 1) / a.per_chunk;
-    const uint32_t units = (uint32_t)a.B * a.N * a.n_tensors * a.chunks;
-    const int groups = heads::kThreads >> a.log_lanes;
+    a.units = heads::units_of((uint32_t)a.B * a.N, a.n_tensors * a.chunks, a.log_lanes);
+    const uint32_t groups = heads::kThreads >> a.log_lanes;
     const Kernel kern = pick<Fwd>(c);
-    kern<<<(units + groups - 1) / groups, heads::kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
+    kern<<<(a.units.all + groups - 1) / groups, heads::kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
     return cudaGetLastError() == cudaSuccess ? HLA_OK : HLA_ERR_CUDA;
 }
 
