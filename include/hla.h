@@ -456,12 +456,23 @@ typedef struct {
     int64_t g_batch_stride, g_token_stride;
 } hla_scan_config;
 hla_status hla_scan_create(const hla_scan_config *cfg, hla_scan **out);
-/* Scratch of both calls (0 where there are channels enough to fill the machine: a long sequence of few channels runs in parts). */
+/*
+ * Scratch of both calls: HLA_SCAN_STATUS_BYTES, and more where a long sequence of few channels runs in parts; only these need it.  A call that
+ * needs none can be given none (NULL, 0), or another one of at least HLA_SCAN_STATUS_BYTES, 256-byte aligned, for its record:
+ * blocks that share a sequence wait for one another for two seconds at most; where a wait runs out the outputs from there on are not numbers, and
+ * the first bytes of the workspace record it.  hla_scan_last_device_status synchronises `cuda_stream`, reads the record, takes it back and returns
+ * HLA_OK, HLA_ERR_DEVICE_TIMEOUT (since it was last read) or HLA_ERR_CUDA.  The record is one value that memory does not hold by chance; memory that
+ * was the workspace of a call that timed out is zeroed before it is one again.  hla_scan_selftest_bounded_wait enqueues a kernel that
+ * waits for a millisecond for what never comes, records it and returns.
+ */
+#define HLA_SCAN_STATUS_BYTES 256u
 size_t hla_scan_workspace_bytes(const hla_scan *ctx);
 hla_status hla_scan_forward(hla_scan *ctx, const void *x, const void *g, const void *h0, void *h, void *h_last, void *workspace, size_t workspace_bytes,
                             void *cuda_stream);
 hla_status hla_scan_backward(hla_scan *ctx, const void *x, const void *g, const void *h0, const void *h, const void *dh, const void *dh_last,
                              void *dx, void *dg, void *dh0, void *workspace, size_t workspace_bytes, void *cuda_stream);
+hla_status hla_scan_last_device_status(hla_scan *ctx, void *workspace, void *cuda_stream);
+hla_status hla_scan_selftest_bounded_wait(hla_scan *ctx, void *workspace, size_t workspace_bytes, void *cuda_stream);
 hla_status hla_scan_destroy(hla_scan *ctx);
 
 const char *hla_status_string(hla_status s);

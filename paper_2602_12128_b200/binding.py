@@ -22,7 +22,8 @@ EXPORTS = [
     "hla_destroy", "hla_status_string",
     "hla_heads_create", "hla_heads_workspace_bytes", "hla_heads_forward", "hla_heads_backward", "hla_heads_destroy",
     "hla_adamw_create", "hla_adamw_set_grads", "hla_adamw_workspace_bytes", "hla_adamw_step", "hla_adamw_destroy",
-    "hla_scan_create", "hla_scan_workspace_bytes", "hla_scan_forward", "hla_scan_backward", "hla_scan_destroy",
+    "hla_scan_create", "hla_scan_workspace_bytes", "hla_scan_forward", "hla_scan_backward",
+    "hla_scan_last_device_status", "hla_scan_selftest_bounded_wait", "hla_scan_destroy",
 ]
 
 
@@ -52,6 +53,7 @@ class HlaWsLayout(ctypes.Structure):
 HLA_PAIR_ADJACENT, HLA_PAIR_HALVES = 0, 1
 HLA_STATE_F32, HLA_STATE_Q8 = 0, 1
 HLA_GATE_LOG, HLA_GATE_SIGMOID = 0, 1
+HLA_SCAN_STATUS_BYTES = 256
 
 
 class HlaHeadsConfig(ctypes.Structure):
@@ -162,6 +164,8 @@ def load_library(rebuild: bool = False) -> ctypes.CDLL:
         "hla_scan_create": [POINTER(HlaScanConfig), POINTER(c_void_p)],
         "hla_scan_forward": [c_void_p] * 7 + [c_size_t, c_void_p],
         "hla_scan_backward": [c_void_p] * 11 + [c_size_t, c_void_p],
+        "hla_scan_last_device_status": [c_void_p, c_void_p, c_void_p],
+        "hla_scan_selftest_bounded_wait": [c_void_p, c_void_p, c_size_t, c_void_p],
         "hla_scan_destroy": [c_void_p],
     }.items():
         getattr(lib, name).argtypes = args
@@ -767,6 +771,8 @@ class Scan(_Owner):
         self._shape, self._state = torch.Size((B, N, C)), torch.Size((B, C))
         self._new, self._new_state = _Maker(self._shape, self.torch_dtype, device), _Maker(self._state, torch.float32, device)
         self._make_workspace("hla_scan_workspace_bytes", device)
+        if self.workspace is not None:
+            self.workspace[:HLA_SCAN_STATUS_BYTES].zero_()
         self._forward, self._backward = load_library().hla_scan_forward, load_library().hla_scan_backward
 
     def _make(self):
@@ -781,7 +787,8 @@ class Scan(_Owner):
             _here(x, "x", dt, shape, device)
             _here(g, "g", dt, shape, device)
         strides = x.stride(), g.stride()
-        self._workspace_here(device)
+        if self._need > HLA_SCAN_STATUS_BYTES:
+            self._workspace_here(device)
         if strides == self._seen:
             return
         B, N, C = self._shape
@@ -800,6 +807,14 @@ class Scan(_Owner):
             self._made_for = want
         self._seen = strides
 
+    def _scratch_on(self, device):
+        """The workspace, but on another device than its own (where it is not needed) none."""
+        return (self._scratch, self._need) if device == self._on else (0, 0)
+
+    def device_status(self, stream=None) -> int:
+        """Synchronises the stream: HLA_OK, or HLA_ERR_DEVICE_TIMEOUT where a wait between blocks has run out since this was last asked."""
+        return int(load_library().hla_scan_last_device_status(self.ctx, self._scratch, _stream(stream)))
+
     def forward(self, x, g, h0=None, h=None, h_last=None, stream=None):
         """h [B,N,C] and the state behind the last token.  h_last may be the tensor h0."""
         dev, f32 = _device(), torch.float32
@@ -807,7 +822,7 @@ class Scan(_Owner):
         h = self._new(dev) if h is None else h
         h_last = self._new_state(dev) if h_last is None else h_last
         st = self._forward(self.ctx, x.data_ptr(), g.data_ptr(), _dense(h0, "h0", f32, self._state, dev), _dense(h, "h", self.torch_dtype, self._shape, dev),
-                           _dense(h_last, "h_last", f32, self._state, dev), self._scratch, self._need, _stream(stream))
+                           _dense(h_last, "h_last", f32, self._state, dev), *self._scratch_on(dev), _stream(stream))
         if st != HLA_OK:
             raise HlaError(st, "hla_scan_forward")
         return h, h_last
@@ -821,7 +836,7 @@ class Scan(_Owner):
         dh0 = self._new_state(dev) if h0 is not None else None
         st = self._backward(self.ctx, x.data_ptr(), g.data_ptr(), _dense(h0, "h0", f32, self._state, dev), _dense(h, "h", dt, shape, dev),
                             _dense(dh, "dh", dt, shape, dev), _dense(dlast, "dlast", f32, self._state, dev), _dense(dx, "dx", dt, shape, dev),
-                            _dense(dg, "dg", dt, shape, dev), 0 if dh0 is None else dh0.data_ptr(), self._scratch, self._need, _stream(stream))
+                            _dense(dg, "dg", dt, shape, dev), 0 if dh0 is None else dh0.data_ptr(), *self._scratch_on(dev), _stream(stream))
         if st != HLA_OK:
             raise HlaError(st, "hla_scan_backward")
         return dx, dg, dh0

@@ -52,7 +52,14 @@ struct Args {
     float* last;                                 // state that goes out (forward h_N, backward dh0), or null
     int segments, summary;                       // parts of a sequence that run side by side; 1: only their maps are wanted
     float2* maps;                                // [segment][B][C] maps of the segments, and the state that comes in
+    unsigned long long* status;                  // becomes kTimedOut when a wait runs out, or null
 };
+// No call clears the record (that would be a launch more, and calls of other streams may be under way): it is a value that memory hardly holds by
+// chance, and reading it takes it back.
+constexpr unsigned long long kTimedOut = 0x8c5f3a9d17e264b1ull;
+__device__ __forceinline__ void record_timeout(unsigned long long* status) {
+    if (status) *status = kTimedOut;
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ uint32_t cluster_blocks() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
@@ -240,7 +247,7 @@ constexpr int kMapsThere = 1, kStatesThere = 2;
 // Every map of a piece is written by its block straight into the shared memory of all blocks of the cluster and counted by their barriers.
 // A buffer is written again two pieces later: by then its writer has had this block's map of the piece between, which this block sends
 // behind its reads of the buffer.
-__device__ __forceinline__ float2 exchange(Exchange& e, int pieces, int rank, int blocks, float carry) {
+__device__ __forceinline__ float2 exchange(Exchange& e, int pieces, int rank, int blocks, float carry, unsigned long long* status) {
     const int lane = threadIdx.x & 31;
     const float *wa = &e.warps_a[0][0].x + lane, *wh = &e.warps_h[0][0].x + lane;
     float* before = &e.before[0][0].x + lane;
@@ -278,6 +285,7 @@ __device__ __forceinline__ float2 exchange(Exchange& e, int pieces, int rank, in
                              : "memory");
         if (!lost && !tc::mbar_wait(&e.full[buffer], (s >> 1) & 1)) {      // (two seconds: the outputs from here on are not numbers)
             lost = true;
+            record_timeout(status);
             carry = __int_as_float(0x7fc00000);
         }
         float2 q[kMaxCluster];
@@ -343,7 +351,7 @@ __device__ __forceinline__ float state_in(const Args& p, int b, int segment) {
 __device__ __forceinline__ void exchange_warp(Exchange& e, const Args& p, int rank, int blocks, int b, int segment, float carry) {
     const int c = blockIdx.y * kTile + (threadIdx.x & 31);
     const size_t at = (size_t)b * p.C + c, all = (size_t)(gridDim.z / p.segments) * p.C;
-    const float2 map = exchange(e, p.pieces, rank, blocks, carry);
+    const float2 map = exchange(e, p.pieces, rank, blocks, carry, p.status);
     if (rank != 0 || c >= p.C) return;
     if (p.summary) {
         p.maps[segment * all + at] = map;
@@ -537,6 +545,14 @@ __global__ void __launch_bounds__(kThreads + 32, BLOCKS) backward_kernel(const _
     cluster_sync();
 }
 
+// Waits, with a limit, for a barrier that nothing arrives at.
+__global__ void wait_selftest_kernel(unsigned long long* status, unsigned long long limit_ns) {
+    __shared__ uint64_t bar;
+    if (threadIdx.x == 0) tc::mbar_init(&bar, 1);
+    __syncwarp();
+    if (!tc::mbar_wait(&bar, 0, limit_ns)) record_timeout(status);
+}
+
 template <typename T> constexpr int forward_bytes() { return kThreads / 32 * 3 * 2 * Stage<T>::kBytes; }
 template <typename T> constexpr int backward_bytes(bool convex) { return kThreads / 32 * 2 * (convex ? 4 : 3) * Stage<T>::kBytes; }
 
@@ -656,11 +672,12 @@ hla_status launch(hla_scan* c, bool back, Kernel kern, int bytes, scan::Args& a,
     int blocks = cluster_of(c);
     auto pieces = [&] { return ((long long)a.N + blocks * piece - 1) / (blocks * piece); };
     a.segments = choose ? 1 : segments_of(c, blocks, pieces());
-    a.maps = static_cast<float2*>(workspace);
     if (a.segments > 1) {
         if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
         if (workspace_bytes < hla_scan_workspace_bytes(c)) return HLA_ERR_WORKSPACE;
+        a.maps = reinterpret_cast<float2*>(static_cast<char*>(workspace) + HLA_SCAN_STATUS_BYTES);
     }
+    if (workspace && !(reinterpret_cast<uintptr_t>(workspace) & 255u) && workspace_bytes >= HLA_SCAN_STATUS_BYTES) a.status = static_cast<unsigned long long*>(workspace);
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return HLA_ERR_CUDA;
     if (c->ready[back] != kern || c->device != dev) {
@@ -726,9 +743,10 @@ hla_status hla_scan_create(const hla_scan_config* cfg, hla_scan** out) {
 }
 
 size_t hla_scan_workspace_bytes(const hla_scan* c) {
-    if (!c || 3 * columns_of(c) > 3ll * c->sm_count) return 0;      // too many channels for segments
+    if (!c) return 0;
+    if (3 * columns_of(c) > 3ll * c->sm_count) return HLA_SCAN_STATUS_BYTES;      // too many channels for segments
     const long long n = 3ll * c->sm_count / columns_of(c);          // (clusters of one block would leave room for as many)
-    return (size_t)((n + 1) * c->cfg.B * c->cfg.C * 8 + 255) / 256 * 256;
+    return HLA_SCAN_STATUS_BYTES + (size_t)((n + 1) * c->cfg.B * c->cfg.C * 8 + 255) / 256 * 256;
 }
 
 hla_status hla_scan_forward(hla_scan* c, const void* x, const void* g, const void* h0, void* h, void* h_last, void* workspace, size_t workspace_bytes,
@@ -782,6 +800,22 @@ hla_status hla_scan_backward(hla_scan* c, const void* x, const void* g, const vo
     a.h0 = static_cast<const float*>(h0);
     a.last = static_cast<float*>(dh0);
     return launch(c, true, many(c) ? pick<BwdMany>(c->cfg, width(c, a)) : pick<Bwd>(c->cfg, width(c, a)), c->cfg.dtype == HLA_BF16 ? scan::backward_bytes<__nv_bfloat16>(c->cfg.convex) : scan::backward_bytes<float>(c->cfg.convex), a, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+}
+
+hla_status hla_scan_last_device_status(hla_scan* c, void* workspace, void* cuda_stream) {
+    if (!c || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    unsigned long long word = 0;
+    if (cudaMemcpyAsync(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return HLA_ERR_CUDA;
+    if (word != scan::kTimedOut) return HLA_OK;
+    return cudaMemsetAsync(workspace, 0, sizeof(word), st) == cudaSuccess ? HLA_ERR_DEVICE_TIMEOUT : HLA_ERR_CUDA;
+}
+
+hla_status hla_scan_selftest_bounded_wait(hla_scan* c, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!c || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
+    if (workspace_bytes < HLA_SCAN_STATUS_BYTES) return HLA_ERR_WORKSPACE;
+    scan::wait_selftest_kernel<<<1, 32, 0, static_cast<cudaStream_t>(cuda_stream)>>>(static_cast<unsigned long long*>(workspace), 1000000ull);      // gives up after 1 ms
+    return cudaGetLastError() == cudaSuccess ? HLA_OK : HLA_ERR_CUDA;
 }
 
 hla_status hla_scan_destroy(hla_scan* c) {
