@@ -643,6 +643,14 @@ bool many(const hla_scan* c) {
     const int blocks = cluster_of(c);
     return blocks < scan::kMaxCluster && blocks * piece_of(c) < c->cfg.N;
 }
+// The parts of a call.
+long long pieces_of(const hla_scan* c, int blocks) { return ((long long)c->cfg.N + blocks * piece_of(c) - 1) / (blocks * piece_of(c)); }
+int parts_of(const hla_scan* c, bool back) {
+    if (back && many(c)) return 1;
+    const int blocks = cluster_of(c);
+    return segments_of(c, blocks, pieces_of(c, blocks));
+}
+
 // With many channels the backward's clusters are those with the least waves x tokens a block, the fewest blocks where it is the same.  Two sequences (three waves of clusters of
 // eight): 195 us, with four blocks (two waves) 200, with two (one) 225; three: 254 with two blocks, 307 with eight; four: 365 with four, 457 with two.
 bool backward_cluster(const hla_scan* c, Kernel kern, int bytes, int& blocks) {
@@ -671,10 +679,8 @@ bool backward_cluster(const hla_scan* c, Kernel kern, int bytes, int& blocks) {
 
 hla_status launch(hla_scan* c, bool back, Kernel kern, int bytes, scan::Args& a, void* workspace, size_t workspace_bytes, cudaStream_t st) {
     const bool choose = back && many(c);
-    const int piece = piece_of(c);
     int blocks = cluster_of(c);
-    auto pieces = [&] { return ((long long)a.N + blocks * piece - 1) / (blocks * piece); };
-    a.segments = choose ? 1 : segments_of(c, blocks, pieces());
+    a.segments = parts_of(c, back);
     if (a.segments > 1) {
         if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
         if (workspace_bytes < hla_scan_workspace_bytes(c)) return HLA_ERR_WORKSPACE;
@@ -691,7 +697,7 @@ hla_status launch(hla_scan* c, bool back, Kernel kern, int bytes, scan::Args& a,
         c->device = dev;
     }
     if (choose) blocks = c->blocks;
-    const long long total = pieces();
+    const long long total = pieces_of(c, blocks);
     a.pieces = (int)((total + a.segments - 1) / a.segments);
     a.segments = (int)((total + a.pieces - 1) / a.pieces);
     cudaLaunchConfig_t cfg = {};
@@ -747,9 +753,8 @@ hla_status hla_scan_create(const hla_scan_config* cfg, hla_scan** out) {
 
 size_t hla_scan_workspace_bytes(const hla_scan* c) {
     if (!c) return 0;
-    if (3 * columns_of(c) > 3ll * c->sm_count) return HLA_SCAN_STATUS_BYTES;      // too many channels for segments
-    const long long n = 3ll * c->sm_count / columns_of(c);          // (clusters of one block would leave room for as many)
-    return HLA_SCAN_STATUS_BYTES + (size_t)((n + 1) * c->cfg.B * c->cfg.C * 8 + 255) / 256 * 256;
+    const size_t parts = parts_of(c, false);      // (the backward has as many or one)
+    return HLA_SCAN_STATUS_BYTES + (parts > 1 ? ((parts + 1) * c->cfg.B * c->cfg.C * sizeof(float2) + 255) / 256 * 256 : 0);
 }
 
 hla_status hla_scan_forward(hla_scan* c, const void* x, const void* g, const void* h0, void* h, void* h_last, void* workspace, size_t workspace_bytes,
