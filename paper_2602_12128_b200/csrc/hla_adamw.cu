@@ -238,7 +238,8 @@ __device__ __forceinline__ uint32_t codes(const P2 (&x)[2], float per, const uin
 __device__ __forceinline__ uint32_t codes_positive(const P2 (&x)[2], float per, const uint32_t* bits) {
     float y[4], s[4];
     scaled(x, per, y);
-    four(x, s);
+    const P2 up[2] = {mul2(x[0], twice(0x1p20f)), mul2(x[1], twice(0x1p20f))};      // (bits of at least 2^20 for whatever is not zero, 2^-149 too)
+    four(up, s);
     uint32_t w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = min(max(__float_as_uint(y[j]), min(__float_as_uint(s[j]), 1u << 20)) * 16u + (bits[j] >> 8), kTop);
