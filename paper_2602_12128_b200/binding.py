@@ -586,6 +586,8 @@ class Heads(_Owner):
             raise ValueError(f"inv_freq: {sum(axes) // 2} values are wanted, not {len(inv_freq)}")
         if float(q_scale) == 0.0 or not theta > 0.0:
             raise ValueError("q_scale must not be 0, and theta must be positive")
+        if norm and float(eps) == 0.0:
+            raise ValueError("eps must not be 0 with norm (the library takes it for 1e-6)")
         three = lambda v: (c_int32 * 3)(*[int(x) for x in v])  # noqa: E731
         freq = (c_double * len(inv_freq))(*[float(f) for f in inv_freq]) if inv_freq is not None else None
         self.torch_dtype = _dtype(dtype)
