@@ -470,6 +470,11 @@ def _dtype(name):
     return _DTYPES[name]
 
 
+def _f32(x) -> float:
+    """What an fp32 field of the library's structures makes of a number: 0 stands for a default in some of them."""
+    return c_float(x).value
+
+
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
@@ -584,10 +589,10 @@ class Heads(_Owner):
             raise ValueError("up to three axes, and a grid of as many")
         if inv_freq is not None and len(inv_freq) != sum(axes) // 2:
             raise ValueError(f"inv_freq: {sum(axes) // 2} values are wanted, not {len(inv_freq)}")
-        if float(q_scale) == 0.0 or not theta > 0.0:
-            raise ValueError("q_scale must not be 0, and theta must be positive")
-        if norm and float(eps) == 0.0:
-            raise ValueError("eps must not be 0 with norm (the library takes it for 1e-6)")
+        if _f32(q_scale) == 0.0 or not theta > 0.0:
+            raise ValueError("q_scale must not be 0 (as fp32), and theta must be positive")
+        if norm and _f32(eps) == 0.0:
+            raise ValueError("eps must not be 0 (as fp32) with norm: the library takes that for 1e-6")
         three = lambda v: (c_int32 * 3)(*[int(x) for x in v])  # noqa: E731
         freq = (c_double * len(inv_freq))(*[float(f) for f in inv_freq]) if inv_freq is not None else None
         self.torch_dtype = _dtype(dtype)
@@ -694,8 +699,8 @@ class AdamW(_Owner):
         for what, v in (("grads", grads), ("ms", ms), ("vs", vs), ("m_scales", m_scales), ("v_scales", v_scales), ("copies", copies), ("weight_decay", decay), ("lr_mul", mul)):
             if v is not None and len(v) != n:
                 raise ValueError(f"{what}: one for each of the {n} params is wanted, not {len(v)}")
-        if any(x == 0.0 for x in mul):
-            raise ValueError("lr_mul must not be 0: leave out tensors that are not trained")
+        if any(_f32(x) == 0.0 for x in mul):
+            raise ValueError("lr_mul must not be 0 (as fp32): leave out tensors that are not trained")
         rows = (HlaAdamwTensor * n)()
         for i, p in enumerate(params):
             if p.dtype not in _CODES or grads[i].dtype not in _CODES:
@@ -737,9 +742,11 @@ class AdamW(_Owner):
     def step(self, lr, step=None, max_norm=0.0, grad_scale=1.0, stream=None):
         """lr: a number, or an fp32 CUDA scalar that the step reads.  step: its number from 1 on (None: counted here), or an int64 CUDA scalar: with
         both on the device a captured step can be replayed with new values."""
-        if grad_scale == 0.0:
-            raise ValueError("grad_scale must not be 0")
         a = HlaAdamwStepArgs(0.0, 1, 0, 0, max_norm, grad_scale, self._norm)
+        if a.grad_scale == 0.0:
+            raise ValueError("grad_scale must not be 0 (as fp32)")
+        if a.max_norm == 0.0 and max_norm != 0.0:
+            raise ValueError(f"max_norm: {max_norm} is 0 as fp32, which stands for no norm")
         if isinstance(lr, torch.Tensor):
             a.lr_device = _dense(lr, "lr", torch.float32)
         else:

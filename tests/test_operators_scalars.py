@@ -1,5 +1,6 @@
 """Scalars of the operators beside the attention that the library would take for something else.  No GPU is needed."""
 import pytest
+import torch
 
 from paper_2602_12128_b200 import binding as b
 
@@ -12,3 +13,25 @@ def test_heads_without_eps_are_refused():
         b.Heads(1, 2, 24, 64, norm=True, eps=0, device=None)
     b.Heads(1, 2, 24, 64, norm=False, eps=0.0, device=None)            # not read
     b.Heads(1, 2, 24, 64, norm=True, eps=1e-30, device=None)
+
+
+TINY = 1e-46        # not 0, but 0 as fp32
+
+
+def test_scalars_that_are_zero_as_fp32_are_refused():
+    """0 as fp32 stands for a default (1e-6, 1, 1, 1) or, as max_norm, for no norm at all."""
+    for kw in (dict(norm=True, eps=TINY), dict(q_scale=TINY), dict(q_scale=-TINY)):
+        with pytest.raises(ValueError):
+            b.Heads(1, 2, 24, 64, device=None, **kw)
+    step = b.AdamW.step.__get__(_Step())
+    for kw in (dict(grad_scale=TINY), dict(max_norm=TINY)):
+        with pytest.raises(ValueError):
+            step(1e-3, **kw)
+    p = [torch.zeros(10)]
+    with pytest.raises(ValueError, match="lr_mul"):
+        b.AdamW(p, [torch.zeros(10)], lr_mul=TINY, device="cpu")
+
+
+class _Step:
+    """What AdamW.step looks at before it refuses."""
+    _norm, steps, _on = 0, 0, -1
