@@ -593,6 +593,9 @@ class Heads(_Owner):
             raise ValueError("q_scale must not be 0 (as fp32), and theta must be positive")
         if norm and _f32(eps) == 0.0:
             raise ValueError("eps must not be 0 (as fp32) with norm: the library takes that for 1e-6")
+        for what, v in (("axes", axes), ("grid", grid or ()), ("start", start)):
+            if any(not -(1 << 31) <= int(x) < 1 << 31 for x in v):      # (ctypes would wrap it round)
+                raise ValueError(f"{what}: 32-bit integers are wanted, not {tuple(v)}")
         three = lambda v: (c_int32 * 3)(*[int(x) for x in v])  # noqa: E731
         freq = (c_double * len(inv_freq))(*[float(f) for f in inv_freq]) if inv_freq is not None else None
         self.torch_dtype = _dtype(dtype)

@@ -15,6 +15,15 @@ def test_heads_without_eps_are_refused():
     b.Heads(1, 2, 24, 64, norm=True, eps=1e-30, device=None)
 
 
+def test_places_beyond_32_bits_are_refused():
+    """They would come out 2^32 away."""
+    make = lambda **kw: b.Heads(1, 2, 24, 64, device=None, **{**dict(axes=(24, 20, 20), grid=(2, 3, 4)), **kw})
+    for kw in (dict(start=(1 << 31, 0, 0)), dict(start=(0, -(1 << 31) - 1, 0)), dict(start=((1 << 32) + 5, 0, 0)), dict(grid=((1 << 32) + 2, 3, 4)), dict(axes=((1 << 32) + 24, 20, 20))):
+        with pytest.raises(ValueError):
+            make(**kw)
+    make(start=(-(1 << 31), (1 << 31) - 4, 0))
+
+
 TINY = 1e-46        # not 0, but 0 as fp32
 
 
