@@ -506,6 +506,12 @@ def _dense(t, what, dtype, shape=None, device=None):
     return t.data_ptr()
 
 
+def _scalar(t, what, dtype):
+    if t.numel() != 1:
+        raise ValueError(f"{what}: one element is wanted, not {t.numel()}")
+    return _dense(t, what, dtype)
+
+
 class _Maker:
     """Makes uninitialised tensors of one shape and type.  torch.empty with size, type and device takes 3.1 us of the host, torch.empty_like of a
     tensor that has the shape but no memory 1.4 us; a call for one token is bound by the host.  (Large ones, to whom a microsecond is nothing and
@@ -715,7 +721,7 @@ class AdamW(_Owner):
                                      count(m_scales[i], "m_scales", torch.float32, rows_of) if q8 else 0, count(v_scales[i], "v_scales", torch.float32, rows_of) if q8 else 0,
                                      size, mul[i], decay[i], _CODES[p.dtype], _CODES[grads[i].dtype])
         self.norm = torch.zeros((), dtype=torch.float32, device=device) if norm is None else norm
-        _dense(self.norm, "norm", torch.float32)
+        _scalar(self.norm, "norm", torch.float32)
         cfg = HlaAdamwConfig(betas[0], betas[1], eps, HLA_STATE_Q8 if q8 else HLA_STATE_F32, seed)
         self.ctx = _create("hla_adamw_create", byref(cfg), rows, n)
         # the library only borrows pointers
@@ -751,11 +757,11 @@ class AdamW(_Owner):
         if a.max_norm == 0.0 and max_norm != 0.0:
             raise ValueError(f"max_norm: {max_norm} is 0 as fp32, which stands for no norm")
         if isinstance(lr, torch.Tensor):
-            a.lr_device = _dense(lr, "lr", torch.float32)
+            a.lr_device = _scalar(lr, "lr", torch.float32)
         else:
             a.lr = lr
         if isinstance(step, torch.Tensor):
-            a.step_device = _dense(step, "step", torch.int64)
+            a.step_device = _scalar(step, "step", torch.int64)
         else:
             a.step = self.steps + 1 if step is None else step
         if self._on != _device():

@@ -44,3 +44,27 @@ def test_scalars_that_are_zero_as_fp32_are_refused():
 class _Step:
     """What AdamW.step looks at before it refuses."""
     _norm, steps, _on = 0, 0, -1
+
+
+@pytest.mark.parametrize("device", ["cpu", pytest.param("cuda", marks=pytest.mark.gpu)])
+def test_a_rate_and_a_number_on_the_device_are_one_element(device):
+    """A tensor without elements has no address, which stood for the number beside it: a rate of 0, the step 1."""
+    step = b.AdamW.step.__get__(_Step())
+    for n in (0, 2):
+        with pytest.raises(ValueError, match="one element"):
+            step(torch.zeros(n, device=device))
+        with pytest.raises(ValueError, match="one element"):
+            step(1e-3, step=torch.zeros(n, dtype=torch.int64, device=device))
+
+
+@pytest.mark.gpu
+def test_the_norm_is_one_element():
+    p, g = [torch.zeros(64, device="cuda")], [torch.ones(64, device="cuda")]
+    for n in (0, 2):
+        with pytest.raises(ValueError, match="one element"):
+            b.AdamW(p, g, norm=torch.zeros(n, device="cuda"))
+    for shape in ((), (1,)):
+        norm, lr, step = torch.zeros(shape, device="cuda"), torch.full(shape, 1e-3, device="cuda"), torch.ones(shape, dtype=torch.int64, device="cuda")
+        opt = b.AdamW(p, g, norm=norm)
+        opt.step(lr, step, max_norm=100.0)
+        assert norm.item() == 8.0
