@@ -580,6 +580,15 @@ bool positions_ok(const hla_heads* c, const int32_t* positions, int64_t pos_batc
     return pos_batch == 0 || (pos_batch >= (int64_t)c->cfg.N * c->cfg.n_axes && pos_batch < (1ll << 40));
 }
 
+// Whether n bytes at `out` share memory with a norm weight or with the positions that a call reads.
+bool over_small_inputs(const hla_heads* c, const void* out, size_t n, const void* wq, const void* wk, const int32_t* positions, int64_t pos_batch) {
+    const size_t weight = (size_t)c->cfg.d * elt_size(c->cfg.dtype);
+    if ((wq && overlap(out, n, wq, weight)) || (wk && overlap(out, n, wk, weight))) return true;
+    if (!positions || !c->rot) return false;
+    const size_t read = ((size_t)(c->cfg.B - 1) * pos_batch + (size_t)c->cfg.N * c->cfg.n_axes) * sizeof(int32_t);
+    return overlap(out, n, positions, read);
+}
+
 bool weight_ok(const hla_heads* c, const void* w) { return !w || (c->cfg.norm && aligned16(w)); }
 
 }  // namespace
@@ -669,6 +678,7 @@ hla_status hla_heads_forward(hla_heads* c, const hla_rows* q, const hla_rows* k,
         if (!in[i] != !to[i]) return HLA_ERR_INVALID_ARG;
         if (!in[i]) continue;
         if (!rows_ok(c, in[i]) || !aligned16(to[i])) return HLA_ERR_INVALID_ARG;
+        if (over_small_inputs(c, to[i], dense, wq, wk, positions, positions_batch_stride)) return HLA_ERR_INVALID_ARG;
         for (int j = 0; j < 3; ++j) {      // an output over an input, or over another output
             if (in[j] && in[j]->data && overlap(to[i], dense, in[j]->data, rows_span(c, in[j]))) return HLA_ERR_INVALID_ARG;
             if (j != i && to[j] && overlap(to[i], dense, to[j], dense)) return HLA_ERR_INVALID_ARG;
