@@ -18,6 +18,7 @@
 // cluster.  Backward of two such sequences, log gates: 200 us, 5.0 TB/s, 30 instructions an element at 47 %.
 #include "../../include/hla.h"
 
+#include <algorithm>
 #include <new>
 #include <type_traits>
 
@@ -34,11 +35,11 @@ template <typename T> constexpr int kRunOf = sizeof(T) == 2 ? 8 : 4;            
 template <typename T> constexpr int kPieceOf = kRuns * kRunOf<T>;               // tokens of a block between two exchanges
 constexpr int kTile = 2 * kLanes;                // channels of a block
 constexpr int kMaxCluster = 8;
-constexpr int kBlocks = 3;                       // on an SM, and of the backward with many channels:
-// With three its time depends on where the clusters come to lie (2 x 32760 x 1536, log gates: 199 to 285 us, with two 197) and its registers do
-// not hold the tokens of a thread (convex, sigmoid gates: 297 us, with two 238).  Where clusters of eight fit at once three are better (32760 x
-// 1536, log gates: 94 us, with two 123).
+constexpr int kBlocks = 3;                       // on an SM, where shared memory has room for them (kBlocksBack), and of the backward with many channels:
+// With three its time depends on where the clusters come to lie (2 x 32760 x 1536, log gates: 199 to 285 us, with two 197).  Where clusters of
+// eight fit at once three are better (32760 x 1536, log gates: 94 us, with two 123).
 constexpr int kBlocksMany = 2;
+constexpr int kSharedOfSm = 228 << 10, kSharedOfRuntime = 1 << 10;      // bytes of shared memory of an SM, and what a block takes beside its own
 
 enum { kLog = 0, kSigmoid = 1 };
 
@@ -559,6 +560,15 @@ __global__ void wait_selftest_kernel(unsigned long long* status, unsigned long l
 template <typename T> constexpr int forward_bytes() { return kThreads / 32 * 3 * 2 * Stage<T>::kBytes; }
 template <typename T> constexpr int backward_bytes(bool convex) { return kThreads / 32 * 2 * (convex ? 4 : 3) * Stage<T>::kBytes; }
 
+// Blocks that shared memory has room for: three, but two of the convex backward of a 16-bit type (four inputs, 73728 bytes of stages a block).
+constexpr int blocks_in_shared(int staged) {
+    return kSharedOfSm / (staged + ((int)sizeof(Exchange) + 127) / 128 * 128 + kSharedOfRuntime);
+}
+template <typename T> constexpr int kBlocksForward = kBlocks < blocks_in_shared(forward_bytes<T>()) ? kBlocks : blocks_in_shared(forward_bytes<T>());
+template <typename T, bool CONVEX> constexpr int kBlocksBack = kBlocks < blocks_in_shared(backward_bytes<T>(CONVEX)) ? kBlocks : blocks_in_shared(backward_bytes<T>(CONVEX));
+static_assert(kBlocksForward<__nv_bfloat16> == kBlocks && kBlocksForward<float> == kBlocks, "what the forward's launch bounds say");
+static_assert(kBlocksBack<__nv_bfloat16, true> >= kBlocksMany && kBlocksBack<float, true> >= kBlocksMany, "what the launch bounds of the backward with many channels say");
+
 }  // namespace scan
 }  // namespace hla
 
@@ -588,7 +598,7 @@ Kernel pick(const hla_scan_config& c, int wide) {
     return wide == 16 ? pick_of<K, __nv_bfloat16, 16>(s, v) : wide == 4 ? pick_of<K, __nv_bfloat16, 4>(s, v) : pick_of<K, __nv_bfloat16, 2>(s, v);
 }
 template <typename T, int GATE, bool CONVEX, int WIDE> struct Fwd { static Kernel get() { return scan::forward_kernel<T, GATE, CONVEX, WIDE>; } };
-template <typename T, int GATE, bool CONVEX, int WIDE> struct Bwd { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX, WIDE, scan::kBlocks>; } };
+template <typename T, int GATE, bool CONVEX, int WIDE> struct Bwd { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX, WIDE, scan::kBlocksBack<T, CONVEX>>; } };
 template <typename T, int GATE, bool CONVEX, int WIDE> struct BwdMany { static Kernel get() { return scan::backward_kernel<T, GATE, CONVEX, WIDE, scan::kBlocksMany>; } };
 
 int elt_size(int dtype) { return dtype == HLA_BF16 ? 2 : 4; }
@@ -615,12 +625,20 @@ int width(const hla_scan* c, const scan::Args& a) {
 
 long long columns_of(const hla_scan* c) { return (long long)((c->cfg.C + scan::kTile - 1) / scan::kTile) * c->cfg.B; }
 
+// Blocks that run at once, as shared memory and launch bounds allow.
+long long places_of(const hla_scan* c, bool back) {
+    const int forward = c->cfg.dtype == HLA_BF16 ? scan::kBlocksForward<__nv_bfloat16> : scan::kBlocksForward<float>;
+    const int convex = c->cfg.dtype == HLA_BF16 ? scan::kBlocksBack<__nv_bfloat16, true> : scan::kBlocksBack<float, true>;
+    const int plain = c->cfg.dtype == HLA_BF16 ? scan::kBlocksBack<__nv_bfloat16, false> : scan::kBlocksBack<float, false>;
+    return (long long)(!back ? forward : c->cfg.convex ? convex : plain) * c->sm_count;
+}
+
 // Parts of a sequence that run side by side: a first pass finds the map of each, and the pass proper starts every part from the states that the
 // maps before it give.  It reads the inputs twice, so it is taken where at least three parts fit on the machine next to one another (75600 tokens:
 // 64 channels 78 us in one part, 29 in 27; 512 channels backward 158 and 131 in three; 32760 tokens of 768 channels 49 and 70 in two, which
 // is not taken).
-int segments_of(const hla_scan* c, int blocks, long long pieces) {
-    long long n = (long long)scan::kBlocks * c->sm_count / (blocks * columns_of(c));
+int segments_of(const hla_scan* c, bool back, int blocks, long long pieces) {
+    long long n = places_of(c, back) / (blocks * columns_of(c));
     if (n > pieces / 2) n = pieces / 2;
     return n < 3 ? 1 : (int)n;
 }
@@ -631,8 +649,8 @@ int piece_of(const hla_scan* c) { return c->cfg.dtype == HLA_BF16 ? scan::kPiece
 // blocks an exchange is shorter.  Forward of 32760 tokens of 1536 channels: two sequences 123 us with four blocks, 133 with eight; three 166 with
 // two, 192 with eight; four 231 with two, 252 with eight.  (Clusters do not fill the groups of SMs that they have to lie in: of eight blocks
 // 48 run at once on 148 SMs, of four 104.)
-int cluster_of(const hla_scan* c) {
-    const long long columns = columns_of(c), room = (long long)scan::kBlocks * c->sm_count;
+int cluster_of(const hla_scan* c, bool back) {
+    const long long columns = columns_of(c), room = places_of(c, back);
     auto fits = [&](int b) { return b * columns <= room - (b == 8 ? room / 8 : b == 4 ? room / 16 : 0); };
     int blocks = 1;
     while (blocks < scan::kMaxCluster && blocks * piece_of(c) < c->cfg.N && fits(2 * blocks)) blocks *= 2;
@@ -640,15 +658,15 @@ int cluster_of(const hla_scan* c) {
 }
 // The backward has many channels where longer clusters would have been of use and found no room.
 bool many(const hla_scan* c) {
-    const int blocks = cluster_of(c);
+    const int blocks = cluster_of(c, true);
     return blocks < scan::kMaxCluster && blocks * piece_of(c) < c->cfg.N;
 }
 // The parts of a call.
 long long pieces_of(const hla_scan* c, int blocks) { return ((long long)c->cfg.N + blocks * piece_of(c) - 1) / (blocks * piece_of(c)); }
 int parts_of(const hla_scan* c, bool back) {
     if (back && many(c)) return 1;
-    const int blocks = cluster_of(c);
-    return segments_of(c, blocks, pieces_of(c, blocks));
+    const int blocks = cluster_of(c, back);
+    return segments_of(c, back, blocks, pieces_of(c, blocks));
 }
 
 // With many channels the backward's clusters are those with the least waves x tokens a block, the fewest blocks where it is the same.  Two sequences (three waves of clusters of
@@ -679,7 +697,7 @@ bool backward_cluster(const hla_scan* c, Kernel kern, int bytes, int& blocks) {
 
 hla_status launch(hla_scan* c, bool back, Kernel kern, int bytes, scan::Args& a, void* workspace, size_t workspace_bytes, cudaStream_t st) {
     const bool choose = back && many(c);
-    int blocks = cluster_of(c);
+    int blocks = cluster_of(c, back);
     a.segments = parts_of(c, back);
     if (a.segments > 1) {
         if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HLA_ERR_INVALID_ARG;
@@ -753,7 +771,7 @@ hla_status hla_scan_create(const hla_scan_config* cfg, hla_scan** out) {
 
 size_t hla_scan_workspace_bytes(const hla_scan* c) {
     if (!c) return 0;
-    const size_t parts = parts_of(c, false);      // (the backward has as many or one)
+    const size_t parts = std::max(parts_of(c, false), parts_of(c, true));
     return HLA_SCAN_STATUS_BYTES + (parts > 1 ? ((parts + 1) * c->cfg.B * c->cfg.C * sizeof(float2) + 255) / 256 * 256 : 0);
 }
 
