@@ -249,13 +249,14 @@ constexpr int kMapsThere = 1, kStatesThere = 2;
 // A buffer is written again two pieces later: by then its writer has had this block's map of the piece between, which this block sends
 // behind its reads of the buffer.
 //
-// A lane whose wait has run out takes no further part (blocks = 0): it neither announces nor sends maps, its outputs from there on are not numbers, and
+// A lane whose wait has run out takes no further part: it neither announces nor sends maps, its outputs from there on are not numbers, and
 // the blocks that wait for it give up as well.  Going on, it would write over maps that others still wait for, arrive twice in one phase of a barrier, or
 // end with maps on their way to it.
 __device__ __forceinline__ float2 exchange(Exchange& e, int pieces, int rank, int blocks, float carry, unsigned long long* status) {
     const int lane = threadIdx.x & 31;
     const float *wa = &e.warps_a[0][0].x + lane, *wh = &e.warps_h[0][0].x + lane;
     float* before = &e.before[0][0].x + lane;
+    bool lost = false;
     float product = 1.f;      // of all factors: (product, carry) is the map of all pieces
     uint32_t there[kMaxCluster], bars[kMaxCluster];      // where this block's maps go in every block, and their barriers
 #pragma unroll
@@ -266,7 +267,7 @@ __device__ __forceinline__ float2 exchange(Exchange& e, int pieces, int rank, in
     }
     for (int s = 0; s < pieces; ++s) {
         const int buffer = s & 1;
-        if (blocks && lane == 0) tc::mbar_arrive_expect_tx(&e.full[buffer], blocks * kTile * (int)sizeof(float2));
+        if (!lost && lane == 0) tc::mbar_arrive_expect_tx(&e.full[buffer], blocks * kTile * (int)sizeof(float2));
         wait_at(kMapsThere);
         float a[kRuns / 2], h[kRuns / 2], PA[kRuns / 2], PH[kRuns / 2], A = 1.f, H = 0.f;
 #pragma unroll
@@ -281,15 +282,17 @@ __device__ __forceinline__ float2 exchange(Exchange& e, int pieces, int rank, in
             H = fmaf(a[w], H, h[w]);
             A *= a[w];
         }
+        if (!lost) {
 #pragma unroll
-        for (int i = 0; i < kMaxCluster; ++i)
-            if (i < blocks)
-                asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(there[i] + buffer * (uint32_t)sizeof(e.blocks[0])), "f"(A), "f"(H),
-                             "r"(bars[i] + buffer * (uint32_t)sizeof(uint64_t))
-                             : "memory");
-        if (blocks && !tc::mbar_wait(&e.full[buffer], (s >> 1) & 1)) {      // (two seconds)
+            for (int i = 0; i < kMaxCluster; ++i)
+                if (i < blocks)
+                    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(there[i] + buffer * (uint32_t)sizeof(e.blocks[0])), "f"(A), "f"(H),
+                                 "r"(bars[i] + buffer * (uint32_t)sizeof(uint64_t))
+                                 : "memory");
+        }
+        if (!lost && !tc::mbar_wait(&e.full[buffer], (s >> 1) & 1)) {      // (two seconds)
             record_timeout(status);
-            blocks = 0;
+            lost = true;
             carry = __int_as_float(0x7fc00000);
         }
         float2 q[kMaxCluster];

@@ -19,11 +19,11 @@ def test_barriers_of_the_scan_are_reached_by_whole_warps():
 
 
 def test_a_block_of_the_scan_whose_wait_ran_out_takes_no_further_part():
-    """Maps that it announced or sent after that would be counted by barriers that are still in an earlier phase.  It has no blocks to send to then."""
+    """Maps that it announced or sent after that would be counted by barriers that are still in an earlier phase."""
     text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "hla_scan.cu")).read())
     start = text.index("float2 exchange(Exchange& e")
     body = text[start:text.index("\n}\n", start)]
     loop = body[body.index("for (int s = 0"):]
-    assert re.search(r"if \(blocks && !tc::mbar_wait\([^{]*\{[^}]*blocks = 0;", loop)
-    assert re.search(r"if \(blocks && lane == 0\) tc::mbar_arrive_expect_tx", loop) and re.search(r"if \(i < blocks\)\s*asm volatile\(\"st\.async", loop)
+    assert re.search(r"if \(!lost && !tc::mbar_wait\([^{]*\{[^}]*lost = true;", loop)
+    assert re.search(r"if \(!lost && lane == 0\) tc::mbar_arrive_expect_tx", loop) and re.search(r"if \(!lost\) \{[^{}]*\"st\.async", loop)
     assert len(re.findall("mbar_wait|mbar_arrive_expect_tx|st\\.async", loop)) == 3
