@@ -540,7 +540,7 @@ class _Owner:
 
     def _make_workspace(self, name, device):
         self._need = int(getattr(load_library(), name)(self.ctx))
-        if device and self._need:
+        if device is not None and self._need:      # (0 is a device)
             self.workspace = torch.empty(self._need, dtype=torch.uint8, device=device)
             self._scratch, self._on = self.workspace.data_ptr(), self.workspace.get_device()
 
