@@ -29,7 +29,9 @@
  *     Each wait gives up after two seconds, and the warps of a block that depend
  *     on one another give up one after the other, so a launch that has timed out
  *     can take several times two seconds to return.
- *   - One ctx must not be used from two host threads at once.
+ *   - One ctx must not be used from two host threads at once.  This holds for the contexts of all
+ *     operators below (hla_heads, hla_adamw, hla_scan), and calls that share a workspace, those
+ *     of captured graphs too, have to follow one another on the device.
  */
 #ifndef HLA_H_
 #define HLA_H_
@@ -423,7 +425,8 @@ typedef struct {
     const int64_t *step_device;  /* device scalar that is read instead of step, or NULL: a captured step can be replayed with new values */
     float max_norm;              /* 0: no norm is taken; infinity: the norm is taken and nothing is clipped */
     float grad_scale;            /* 0 -> 1                                                             */
-    float *norm;                 /* device scalar that receives the norm (max_norm > 0), or NULL       */
+    float *norm;                 /* device scalar that receives the norm (max_norm > 0), or NULL; the three scalars and the workspace
+                                    lie apart from the tensors of the list                             */
 } hla_adamw_step_args;
 
 /* The pointers (16-byte aligned) are remembered; nothing that a step writes may share memory with another tensor of the list. */

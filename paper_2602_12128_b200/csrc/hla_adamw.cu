@@ -3,8 +3,9 @@
 //     m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2,   p' = p - lr wd p - lr / (1 - b1^t) m' / (sqrt(v' / (1 - b2^t)) + eps)
 //
 // What bounds it: with fp32 moments memory (28 bytes an element with fp32 weights, their bf16 copies and bf16 gradients: 227 M elements in
-// 1018 us, 6.24 TB/s, and 79 us for the norm's pass over the gradients).  With 8-bit moments and bf16 weights (10 bytes) the arithmetic: 54
-// instructions an element, 21 of them on the integer pipe, which takes one every other cycle: 490 us, where the bytes would take 353.
+// 1018 to 1042 us, 6.1 to 6.2 TB/s, and 70 to 79 us for the norm's pass over the gradients).  With 8-bit moments and bf16 weights (10 bytes) 54 instructions an
+// element, 21 of them on the integer pipe, which takes one every other cycle: 490 us, where the bytes would take 353.  No unit is at its limit there
+// (issue slots 73 %, integer pipe 55 %, DRAM 55 %).
 //
 // Layout: a row is 128 consecutive elements of a tensor, which is also what shares a scale.  A warp takes two rows, four elements of each a lane (with
 // fp32 moments, so that every load is contiguous) or eight of one (8-bit moments).  Tensors from a few weights to
@@ -75,6 +76,8 @@ struct Args {
     Tensor t[MANY];
 };
 
+// A mixing function of 32 bits: two rounds of xor-shift and multiplication, shifts and factors those of Wellons' "lowbias32" (Hash Prospector),
+// which were searched for the least bias between input and output bits.
 __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
     x ^= x >> 16;
     x *= 0x7FEB352Du;
@@ -189,6 +192,10 @@ __device__ __forceinline__ float max_abs(float a, float b, float c) {      // a 
     return r;
 }
 
+// Root and reciprocal of the update are the hardware's approximations, off by a unit or two in the last place of an update that is small against its
+// weight and has some ten roundings anyway.  Correctly rounded ones are sequences of instructions; the moments, which are what is kept, have
+// neither.
+//
 // Roots of second moments.  SMALL: of those below the smallest normal number too, which a tiny eps does not cover.
 template <bool SMALL>
 __device__ __forceinline__ float sqrt_fast(float x) {

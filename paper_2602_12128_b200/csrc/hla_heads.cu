@@ -140,8 +140,9 @@ struct Place {
     }
 };
 
-// cos and sin of a lane's pairs at token n of batch b, times `scale`.  The angle is reduced to a fraction of a turn in 64 bits: at
-// position 2^31 its error is below 2^-22 turns.
+// cos and sin of a lane's pairs at token n of batch b, times `scale`.  The angle is reduced to a fraction of a turn in 64 bits and the fraction, at
+// most half a turn, rounded to fp32: 2^-26 turns, 9.4e-8 of the pair's length, hardly more than one of the roundings behind it (2^-24, 6e-8), and one
+// sincospi in fp32 will do.  At position 2^31 the product's own rounding in 64 bits adds up to 2^-25 turns (frequencies up to 1).
 template <typename T, bool HALF>
 __device__ __forceinline__ void angles(const Args& p, const double* turns, int l, int b, int n, float scale, P2 (&c)[Vec<T, HALF>::NQ], P2 (&s)[Vec<T, HALF>::NQ]) {
     constexpr int NP = Vec<T, HALF>::NP;
@@ -410,7 +411,8 @@ __global__ void __launch_bounds__(kThreads, 3) backward_kernel(const __grid_cons
         }
     }
     if (NORM && p.want_dw && rotate) {      // (uniform over the block)
-        // group after group: sums[group][channel]
+        // Group after group: sums[group][channel].  A thread's rows (a few hundred) and the groups of a block (at most 256) are summed in fp32, the blocks in 64
+        // bits (dw_kernel): a thread has eight sums and 80 registers in all, and in fp32 the error stays within 2^-24 a row of the sum of the magnitudes.
         constexpr int CH = V::CH;
         float* mine = sums + (size_t)group * CH * (1 << log_lanes);
         if (at.in) {
@@ -476,12 +478,13 @@ namespace {
 
 int elt_size(int dtype) { return dtype == HLA_BF16 ? 2 : 4; }
 
-// Tokens of the grid-stride loop that one block of the backward takes at a time, and how many blocks share the tokens.
+// How many blocks of the backward share the tokens, of `y` runs of heads.
 int backward_blocks(const hla_heads* c, int y) {
     const long long tokens = (long long)c->cfg.B * c->cfg.N;
     const int groups = heads::kThreads >> c->log_lanes;
     const long long tiles = (tokens + groups - 1) / groups;
-    // four waves of four resident blocks: V's blocks, which read half as much, make room early
+    // 16 blocks an SM in all, of which three run at once: V's blocks, which read half as much, and those with fewer tokens make room early.
+    // 2 x 24 x 32760 rows: 492 us; with 12, four whole waves, 495 to 497 (without norm 190 and 192).
     const long long want = (16ll * c->sm_count + y - 1) / y;
     return (int)(tiles < want ? tiles : want);
 }

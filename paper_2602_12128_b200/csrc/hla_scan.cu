@@ -11,11 +11,12 @@
 // composes those of its runs; a cluster of up to eight blocks takes neighbouring pieces of the sequence and hands the maps of its blocks
 // round through distributed shared memory, once for every kPieceOf tokens of a block.  The tokens stay in registers meanwhile and are gone
 // through once more from the state that comes in; the next pieces are on their way into shared memory.  All orders are fixed: results
-// do not depend on timing.  States, maps and sums are fp32.
+// do not depend on timing.  (Where the sequence is cut can depend on the GPU: the clusters that fit on it are counted.)  States, maps and sums are fp32.
 //
-// Forward of 32760 tokens, 1536 channels, bf16, sigmoid gates, convex: 70 us, 4.3 TB/s of 6.5, 24.5 instructions an element, 54 % of the issue
-// slots.  The rest is the wait for the slowest block of a cluster (384 blocks on 148 SMs: three on some, two on others) and the round through the
-// cluster.  Backward of two such sequences, log gates: 200 us, 5.0 TB/s, 30 instructions an element at 47 %.
+// Forward of 32760 tokens, 1536 channels, bf16, sigmoid gates, convex: 70 to 74 us from GPU to GPU, 4.1 to 4.3 TB/s of 6.5, 24.5 instructions an
+// element, 54 % of the issue slots.  The rest is the wait for the slowest block of a cluster (384 blocks on 148 SMs: three on some, two on others) and the round
+// through the cluster.  Backward of two such sequences, log gates: 197 to 216 us, 4.7 to 5.1 TB/s, 30 instructions an element at 47 %; of one, sigmoid
+// gates, convex: 147 us, 4.1 TB/s, two blocks an SM in 192 blocks of clusters of four.
 #include "../../include/hla.h"
 
 #include <algorithm>
