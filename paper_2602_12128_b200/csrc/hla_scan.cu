@@ -16,7 +16,7 @@
 // Forward of 32760 tokens, 1536 channels, bf16, sigmoid gates, convex: 70 to 74 us from GPU to GPU, 4.1 to 4.3 TB/s of 6.5, 24.5 instructions an
 // element, 54 % of the issue slots.  The rest is the wait for the slowest block of a cluster (384 blocks on 148 SMs: three on some, two on others) and the round
 // through the cluster.  Backward of two such sequences, log gates: 197 to 216 us, 4.7 to 5.1 TB/s, 30 instructions an element at 47 %; of one, sigmoid
-// gates, convex: 147 us, 4.1 TB/s, two blocks an SM in 192 blocks of clusters of four.
+// gates, convex: 147 to 151 us, 4.0 to 4.1 TB/s, two blocks an SM in 192 blocks of clusters of four.
 #include "../../include/hla.h"
 
 #include <algorithm>
